@@ -17,6 +17,12 @@
  *                      the masked patches, and its gradient with respect to the prediction.
  *   mae_patch_embed    linear patch embedding of the visible tokens with bias and positional
  *                      embedding (Sec. 2, Sec. 5), on the matrix cores.
+ * The operators that a training step needs around the encoder's blocks, each with its gradient:
+ *   mae_patch_embed_grad  gradients of the embedding's weight, bias and positional rows
+ *   mae_dropout           dropout and drop path from the keyed draws, no mask stored
+ *   mae_layer_norm        layer norm of token rows (mae_layer_norm_grad: its backward pass)
+ *   mae_class_loss        softmax cross entropy of a linear head over many classes, with label
+ *                         smoothing, without keeping the logits
  * mae_prep_batch also takes JPEG files and decodes only the region each crop needs ("crop
  * decode", Sec. 4.1; mae_jpeg_index prepares files once for it) and applies the finetuning
  * augmentation (Sec. 4.4); mae_normpix_loss_from_images is the loss without a stored target;
@@ -335,6 +341,141 @@ typedef struct {
 
 /* Output (device): tokens [M, E] out_dtype, every element written.  No workspace. */
 int mae_patch_embed(const mae_embed_desc* d, void* tokens, void* hip_stream);
+
+/* Gradients of mae_patch_embed: with g = grad_tokens [M, E] bf16, the derivative of the loss with
+ * respect to `tokens`,
+ *   grad_weight[e, d] = sum_m g[m, e] visible[m, d]
+ *   grad_bias[e]      = sum_m g[m, e]
+ *   grad_pos[l, e]    = sum over the rows m with ids_keep[m] = l (clamped as above) of g[m, e]; rows
+ *                       of patches that no token names become 0
+ * The products are exact in single precision; sums are kept in single precision or better, in a fixed
+ * order (two calls give the same bits).  `weight`, `bias` and the values of `pos` are not read.
+ *
+ * Limits: those of mae_patch_embed, out_dtype = MAE_BF16 (MAE_ERR_DTYPE otherwise), and with `pos`
+ * L <= 8192.  grad_tokens and grad_weight are 16-byte aligned.
+ *   grad_weight [E, D] float, grad_bias [E] float, grad_pos [L, E] float    each nullable, not all;
+ *                                           grad_pos only with `pos` in the descriptor
+ *   workspace   mae_patch_embed_grad_workspace_bytes(d) bytes, 256-byte aligned (0: invalid descriptor) */
+int mae_patch_embed_grad(const mae_embed_desc* d, const void* grad_tokens, float* grad_weight, float* grad_bias,
+                         float* grad_pos, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+size_t mae_patch_embed_grad_workspace_bytes(const mae_embed_desc* d);
+
+/* ------------------------------------------------------------------------------------------------
+ * mae_dropout
+ *
+ * Dropout of M rows of D values, and of whole groups of rows ("drop path": a residual branch is left
+ * out for some samples), without a mask in memory: the keyed draws are made again where they are needed.
+ * Value number i = (row_base + row) * D + column -- or, with rows_per_draw = r > 0, group number
+ * i = (row_base + row) / r -- draws 32 bits: the low (i even) or high (i odd) half of
+ *   mix64(key + GAMMA * (i / 2 + 1)),
+ * with mix64 and GAMMA of SplitMix64 and a key made of seed, batch_index and layer.  It is kept iff
+ * the draw >= p * 2^32 (rounded), and
+ *   y = (kept ? x / (1 - p) : 0) + residual
+ * in single precision, rounded once.  What is dropped is selected away, so an infinity or a NaN there
+ * does not reach y.  p = 0 keeps everything, p = 1 drops everything.
+ * The backward pass is the same call with x = the gradient of y and residual = NULL: it writes the
+ * gradient of x (that of the residual is the gradient of y itself).
+ *
+ * Limits: 1 <= M <= 2^28, 1 <= D <= 8192, row_base <= 2^48.  Pointers are aligned to their values; y may
+ * be the same memory as x or residual.
+ * ---------------------------------------------------------------------------------------------- */
+typedef struct {
+  int64_t M;
+  int32_t D;
+  const void* x;        /* [M, D] dtype                                                         */
+  const void* residual; /* [M, D] dtype, nullable                                               */
+  int32_t dtype;        /* mae_dtype of x, residual and y                                       */
+  float p;              /* probability to drop, in [0, 1]                                       */
+  int32_t rows_per_draw; /* 0: every value draws; r > 0: r consecutive rows share one draw (the
+                           tokens of one sample)                                                */
+  uint64_t seed;        /* random-number key                                                    */
+  uint64_t batch_index; /* random-number key; vary per step                                     */
+  uint32_t layer;       /* random-number key; vary per place in the model                       */
+  uint64_t row_base;    /* global number of row 0 (0 unless a batch is split)                   */
+} mae_dropout_desc;
+
+int mae_dropout(const mae_dropout_desc* d, void* y, void* hip_stream);
+
+/* ------------------------------------------------------------------------------------------------
+ * mae_layer_norm
+ *
+ * For every row x of D values: mean, rstd = 1 / sqrt(mean((x - mean)^2) + eps), h = (x - mean) rstd,
+ *   y = h * weight + bias
+ * Statistics are single precision, from two passes over registers.  Backward, with G = grad_y * weight:
+ *   grad_x = rstd (G - mean(G) - h mean(G h)),  grad_weight = sum over rows of grad_y h,
+ *   grad_bias = sum over rows of grad_y
+ * The sums over rows have a fixed order (two calls give the same bits).
+ *
+ * Limits: 1 <= M <= 2^28, 1 <= D <= 8192.  Pointers are aligned to their values.  y may be the same
+ * memory as x, and grad_x as x or grad_y, where the types are the same.
+ * ---------------------------------------------------------------------------------------------- */
+typedef struct {
+  int64_t M;
+  int32_t D;
+  const void* x;       /* [M, D] x_dtype                                                        */
+  const float* weight; /* [D], nullable (ones)                                                  */
+  const float* bias;   /* [D], nullable (zeros); not read by the backward pass                  */
+  float eps;           /* >= 0, 1e-6 in the MAE recipe                                          */
+  int32_t x_dtype;     /* mae_dtype of x and grad_x                                             */
+  int32_t y_dtype;     /* mae_dtype of y and grad_y                                             */
+} mae_norm_desc;
+
+/*   y [M, D] y_dtype  required;  mean, rstd [M] float  nullable (what the backward pass takes) */
+int mae_layer_norm(const mae_norm_desc* d, void* y, float* mean, float* rstd, void* hip_stream);
+
+/*   grad_y, mean, rstd  required
+ *   grad_x [M, D] x_dtype, grad_weight [D] float, grad_bias [D] float    each nullable, not all
+ *   workspace  mae_layer_norm_workspace_bytes(d) bytes, 256-byte aligned; required with grad_weight or
+ *              grad_bias, else not used */
+int mae_layer_norm_grad(const mae_norm_desc* d, const void* grad_y, const float* mean, const float* rstd, void* grad_x,
+                        float* grad_weight, float* grad_bias, void* workspace, size_t workspace_bytes,
+                        void* hip_stream);
+
+size_t mae_layer_norm_workspace_bytes(const mae_norm_desc* d);
+
+/* ------------------------------------------------------------------------------------------------
+ * mae_class_loss
+ *
+ * The finetuning objective (Sec. 3, Sec. 5.2): a linear head over V classes and the softmax cross
+ * entropy of its logits, with label smoothing s, and the gradients.  For the rows whose label is a class
+ * (0 <= label < V), n of them:
+ *   l = tokens weight^T + bias
+ *   row_loss = lse(l) - (1 - s) l[label] - s mean(l),  loss = sum of row_loss / n
+ *   g = (softmax(l) - (1 - s) onehot(label) - s / V) * grad_scale / n
+ *   grad_tokens = g weight,  grad_weight = g^T tokens,  grad_bias = sum over rows of g
+ * Rows with any other label (-1, say) are left out: their row_loss and grad_tokens are 0, and nothing that
+ * such a row of `tokens` holds is used.  With no row left, loss and gradients are 0.  The logits are never
+ * stored: they are made tile by tile, and once more for the gradient, which goes through the classes in
+ * pieces.  Operands are bf16, logits, maxima and sums single precision, the sum of row_loss double; before the
+ * factor grad_scale / n, g is rounded to fp16 (of 2^15 g) as an operand of the two products, whose other operand
+ * then is an fp16 copy scaled by a power of two: exact for values down to 2^-32 of the tensor's largest.
+ * grad_bias is summed before that rounding.  A class whose bias is -infinity or the lowest float has probability 0.
+ *
+ * Limits: 1 <= M <= 2^24, 8 <= D <= 8192 with D % 8 == 0, 1 <= V <= 2^20, M * V <= 2^38.
+ * tokens, weight, grad_tokens and grad_weight are 16-byte aligned.
+ * ---------------------------------------------------------------------------------------------- */
+typedef struct {
+  int64_t M;
+  int32_t D, V;
+  const void* tokens;    /* [M, D] bf16                                                         */
+  const void* weight;    /* [V, D] bf16                                                         */
+  const float* bias;     /* [V] float, nullable                                                 */
+  const int32_t* labels; /* [M]                                                                 */
+  float smoothing;       /* s in [0, 1]                                                         */
+  float grad_scale;      /* upstream derivative of the loss, normally 1                         */
+} mae_class_desc;
+
+/*   loss [1] float                required
+ *   row_loss [M] float            nullable
+ *   grad_tokens [M, D] bf16, grad_weight [V, D] bf16, grad_bias [V] float   each nullable; grad_bias
+ *                                 only with `bias`
+ *   workspace   mae_class_loss_workspace_bytes(d, with_grad) bytes, 256-byte aligned; with_grad: any of the
+ *               three gradients is wanted (0: invalid descriptor) */
+int mae_class_loss(const mae_class_desc* d, float* loss, float* row_loss, void* grad_tokens, void* grad_weight,
+                   float* grad_bias, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+size_t mae_class_loss_workspace_bytes(const mae_class_desc* d, int32_t with_grad);
 
 /* ------------------------------------------------------------------------------------------------
  * Progressive schedules (host-side tables; nothing is launched).

@@ -32,7 +32,10 @@ EXPORTS = ("mae_prep_batch", "mae_prep_workspace_bytes", "mae_prep_status", "mae
            "mae_jpeg_index", "mae_jpeg_index_bytes",
            "mae_normpix_loss", "mae_loss_workspace_bytes", "mae_normpix_loss_static",
            "mae_normpix_loss_from_images",
-           "mae_loss_from_images_workspace_bytes", "mae_patch_embed", "mae_pretrain_stage",
+           "mae_loss_from_images_workspace_bytes", "mae_patch_embed",
+           "mae_patch_embed_grad", "mae_patch_embed_grad_workspace_bytes", "mae_dropout",
+           "mae_layer_norm", "mae_layer_norm_grad", "mae_layer_norm_workspace_bytes",
+           "mae_class_loss", "mae_class_loss_workspace_bytes", "mae_pretrain_stage",
            "mae_finetune_stage", "mae_stage_of_epoch", "mae_error_string", "mae_version")
 
 
@@ -100,6 +103,49 @@ class MaeEmbedDesc(C.Structure):
     ]
 
 
+class MaeDropoutDesc(C.Structure):
+    _fields_ = [
+        ("M", C.c_int64),
+        ("D", C.c_int32),
+        ("x", C.c_void_p),
+        ("residual", C.c_void_p),
+        ("dtype", C.c_int32),
+        ("p", C.c_float),
+        ("rows_per_draw", C.c_int32),
+        ("seed", C.c_uint64),
+        ("batch_index", C.c_uint64),
+        ("layer", C.c_uint32),
+        ("row_base", C.c_uint64),
+    ]
+
+
+class MaeNormDesc(C.Structure):
+    _fields_ = [
+        ("M", C.c_int64),
+        ("D", C.c_int32),
+        ("x", C.c_void_p),
+        ("weight", C.c_void_p),
+        ("bias", C.c_void_p),
+        ("eps", C.c_float),
+        ("x_dtype", C.c_int32),
+        ("y_dtype", C.c_int32),
+    ]
+
+
+class MaeClassDesc(C.Structure):
+    _fields_ = [
+        ("M", C.c_int64),
+        ("D", C.c_int32),
+        ("V", C.c_int32),
+        ("tokens", C.c_void_p),
+        ("weight", C.c_void_p),
+        ("bias", C.c_void_p),
+        ("labels", C.c_void_p),
+        ("smoothing", C.c_float),
+        ("grad_scale", C.c_float),
+    ]
+
+
 class MaeError(RuntimeError):
     def __init__(self, status: int, where: str):
         self.status = status
@@ -148,6 +194,21 @@ def load():
                                                              C.POINTER(MaeLossDesc)]
         lib.mae_patch_embed.restype = C.c_int
         lib.mae_patch_embed.argtypes = [C.POINTER(MaeEmbedDesc), C.c_void_p, C.c_void_p]
+        p = C.c_void_p
+        for name, args in (
+                ("mae_patch_embed_grad", [C.POINTER(MaeEmbedDesc)] + [p] * 5 + [C.c_size_t, p]),
+                ("mae_dropout", [C.POINTER(MaeDropoutDesc), p, p]),
+                ("mae_layer_norm", [C.POINTER(MaeNormDesc)] + [p] * 4),
+                ("mae_layer_norm_grad", [C.POINTER(MaeNormDesc)] + [p] * 7 + [C.c_size_t, p]),
+                ("mae_class_loss", [C.POINTER(MaeClassDesc)] + [p] * 6 + [C.c_size_t, p])):
+            getattr(lib, name).restype = C.c_int
+            getattr(lib, name).argtypes = args
+        for name, args in (
+                ("mae_patch_embed_grad_workspace_bytes", [C.POINTER(MaeEmbedDesc)]),
+                ("mae_layer_norm_workspace_bytes", [C.POINTER(MaeNormDesc)]),
+                ("mae_class_loss_workspace_bytes", [C.POINTER(MaeClassDesc), C.c_int32])):
+            getattr(lib, name).restype = C.c_size_t
+            getattr(lib, name).argtypes = args
         lib.mae_pretrain_stage.restype = C.c_int
         lib.mae_pretrain_stage.argtypes = [C.c_int32, C.c_int32, C.POINTER(C.c_int32),
                                            C.POINTER(C.c_double)]
@@ -434,6 +495,174 @@ def mae_patch_embed(desc: MaeEmbedDesc, tokens, stream=None) -> None:
     rc = load().mae_patch_embed(C.byref(desc), _ptr(tokens), _stream(stream))
     if rc != MAE_OK:
         raise MaeError(rc, "mae_patch_embed")
+
+
+# ------------------------------------------------------------------------------------------------
+# Operators around the encoder.  Their descriptors hold on to the tensors that they point to.
+# ------------------------------------------------------------------------------------------------
+_FLOATS = (torch.float32, torch.bfloat16)
+
+
+def _mae_dtype(t):
+    return MAE_BF16 if t.dtype == torch.bfloat16 else MAE_F32
+
+
+def _torch_dtype(dtype):
+    return torch.bfloat16 if dtype == MAE_BF16 else torch.float32
+
+
+def _one_device(*tensors, stream=None):
+    """Kernels run on the current device: every tensor (and the stream) has to belong to it."""
+    here = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.device.index != here:
+            raise ValueError(f"tensor on {t.device}, but the current device is cuda:{here}")
+    if stream is not None and stream.device.index != here:
+        raise ValueError(f"stream of {stream.device}, but the current device is cuda:{here}")
+
+
+def _bytes_of(t):
+    return 0 if t is None else t.numel() * t.element_size()
+
+
+def mae_patch_embed_grad_workspace_bytes(desc: MaeEmbedDesc) -> int:
+    return int(load().mae_patch_embed_grad_workspace_bytes(C.byref(desc)))
+
+
+def mae_patch_embed_grad(desc: MaeEmbedDesc, grad_tokens, grad_weight=None, grad_bias=None,
+                         grad_pos=None, workspace=None, stream=None) -> None:
+    """Gradients of mae_patch_embed (the descriptor of that call, out_dtype = MAE_BF16)."""
+    _check(grad_tokens, "grad_tokens", torch.bfloat16, numel=desc.M * desc.E)
+    _check(grad_weight, "grad_weight", torch.float32, numel=desc.E * desc.D, optional=True)
+    _check(grad_bias, "grad_bias", torch.float32, numel=desc.E, optional=True)
+    _check(grad_pos, "grad_pos", torch.float32, numel=desc.L * desc.E, optional=True)
+    _check(workspace, "workspace", optional=True)
+    _one_device(grad_tokens, grad_weight, grad_bias, grad_pos, workspace, stream=stream)
+    rc = load().mae_patch_embed_grad(C.byref(desc), _ptr(grad_tokens), _ptr(grad_weight),
+                                     _ptr(grad_bias), _ptr(grad_pos), _ptr(workspace),
+                                     _bytes_of(workspace), _stream(stream))
+    if rc != MAE_OK:
+        raise MaeError(rc, "mae_patch_embed_grad")
+
+
+def make_dropout_desc(x, residual=None, *, p, rows_per_draw=0, seed=0, batch_index=0, layer=0,
+                      row_base=0) -> MaeDropoutDesc:
+    """x, residual [..., D] float32 or bf16 of one type.  rows_per_draw: 0 = dropout of values, r =
+    drop path, r consecutive rows (the tokens of a sample) sharing a draw."""
+    _check(x, "x", _FLOATS)
+    if x.dim() < 1 or x.shape[-1] < 1:
+        raise ValueError("x must have shape [..., D]")
+    _check(residual, "residual", x.dtype, numel=x.numel(), optional=True)
+    d = MaeDropoutDesc()
+    d.D = int(x.shape[-1])
+    d.M = x.numel() // d.D
+    d.x, d.residual, d.dtype = x.data_ptr(), _ptr(residual), _mae_dtype(x)
+    d.p, d.rows_per_draw = p, rows_per_draw
+    d.seed, d.batch_index, d.layer, d.row_base = seed, batch_index, layer, row_base
+    d.tensors = (x, residual)
+    return d
+
+
+def mae_dropout(desc: MaeDropoutDesc, y, stream=None) -> None:
+    """y = dropped x + residual.  Backward: the same keys with x = the gradient, no residual."""
+    _check(y, "y", _torch_dtype(desc.dtype), numel=desc.M * desc.D)
+    _one_device(y, *desc.tensors, stream=stream)
+    rc = load().mae_dropout(C.byref(desc), _ptr(y), _stream(stream))
+    if rc != MAE_OK:
+        raise MaeError(rc, "mae_dropout")
+
+
+def make_norm_desc(x, weight=None, bias=None, *, eps=1e-6, y_dtype=None) -> MaeNormDesc:
+    """x [..., D] float32 or bf16, weight and bias [D] float32; y_dtype: that of x unless given."""
+    _check(x, "x", _FLOATS)
+    if x.dim() < 1 or x.shape[-1] < 1:
+        raise ValueError("x must have shape [..., D]")
+    _check(weight, "weight", torch.float32, numel=int(x.shape[-1]), optional=True)
+    _check(bias, "bias", torch.float32, numel=int(x.shape[-1]), optional=True)
+    d = MaeNormDesc()
+    d.D = int(x.shape[-1])
+    d.M = x.numel() // d.D
+    d.x, d.weight, d.bias, d.eps = x.data_ptr(), _ptr(weight), _ptr(bias), eps
+    d.x_dtype = _mae_dtype(x)
+    d.y_dtype = d.x_dtype if y_dtype is None else y_dtype
+    d.tensors = (x, weight, bias)
+    return d
+
+
+def mae_layer_norm(desc: MaeNormDesc, y, mean=None, rstd=None, stream=None) -> None:
+    _check(y, "y", _torch_dtype(desc.y_dtype), numel=desc.M * desc.D)
+    _check(mean, "mean", torch.float32, numel=desc.M, optional=True)
+    _check(rstd, "rstd", torch.float32, numel=desc.M, optional=True)
+    _one_device(y, mean, rstd, *desc.tensors, stream=stream)
+    rc = load().mae_layer_norm(C.byref(desc), _ptr(y), _ptr(mean), _ptr(rstd), _stream(stream))
+    if rc != MAE_OK:
+        raise MaeError(rc, "mae_layer_norm")
+
+
+def mae_layer_norm_workspace_bytes(desc: MaeNormDesc) -> int:
+    return int(load().mae_layer_norm_workspace_bytes(C.byref(desc)))
+
+
+def mae_layer_norm_grad(desc: MaeNormDesc, grad_y, mean, rstd, grad_x=None, grad_weight=None,
+                        grad_bias=None, workspace=None, stream=None) -> None:
+    """mean, rstd: as mae_layer_norm wrote them.  workspace: with grad_weight or grad_bias."""
+    _check(grad_y, "grad_y", _torch_dtype(desc.y_dtype), numel=desc.M * desc.D)
+    _check(mean, "mean", torch.float32, numel=desc.M)
+    _check(rstd, "rstd", torch.float32, numel=desc.M)
+    _check(grad_x, "grad_x", _torch_dtype(desc.x_dtype), numel=desc.M * desc.D, optional=True)
+    _check(grad_weight, "grad_weight", torch.float32, numel=desc.D, optional=True)
+    _check(grad_bias, "grad_bias", torch.float32, numel=desc.D, optional=True)
+    _check(workspace, "workspace", optional=True)
+    _one_device(grad_y, mean, rstd, grad_x, grad_weight, grad_bias, workspace, *desc.tensors,
+                stream=stream)
+    rc = load().mae_layer_norm_grad(C.byref(desc), _ptr(grad_y), _ptr(mean), _ptr(rstd),
+                                    _ptr(grad_x), _ptr(grad_weight), _ptr(grad_bias),
+                                    _ptr(workspace), _bytes_of(workspace), _stream(stream))
+    if rc != MAE_OK:
+        raise MaeError(rc, "mae_layer_norm_grad")
+
+
+def make_class_desc(tokens, labels, weight, bias=None, *, smoothing=0.0,
+                    grad_scale=1.0) -> MaeClassDesc:
+    """tokens [..., D] bf16, labels [...] int32 (rows whose label is no class are left out),
+    weight [V, D] bf16, bias [V] float32."""
+    _check(tokens, "tokens", torch.bfloat16)
+    _check(weight, "weight", torch.bfloat16)
+    if tokens.dim() < 1 or weight.dim() != 2 or weight.shape[1] != tokens.shape[-1]:
+        raise ValueError("weight must have shape [V, D] with D = tokens.shape[-1]")
+    if tokens.shape[-1] < 1:
+        raise ValueError("tokens must have shape [..., D]")
+    d = MaeClassDesc()
+    d.D, d.V = int(weight.shape[1]), int(weight.shape[0])
+    d.M = tokens.numel() // d.D
+    _check(labels, "labels", torch.int32, numel=d.M)
+    _check(bias, "bias", torch.float32, numel=d.V, optional=True)
+    d.tokens, d.weight = tokens.data_ptr(), weight.data_ptr()
+    d.bias, d.labels = _ptr(bias), labels.data_ptr()
+    d.smoothing, d.grad_scale = smoothing, grad_scale
+    d.tensors = (tokens, labels, weight, bias)
+    return d
+
+
+def mae_class_loss_workspace_bytes(desc: MaeClassDesc, with_grad=True) -> int:
+    return int(load().mae_class_loss_workspace_bytes(C.byref(desc), 1 if with_grad else 0))
+
+
+def mae_class_loss(desc: MaeClassDesc, loss, row_loss=None, grad_tokens=None, grad_weight=None,
+                   grad_bias=None, workspace=None, stream=None) -> None:
+    _check(loss, "loss", torch.float32, numel=1)
+    _check(row_loss, "row_loss", torch.float32, numel=desc.M, optional=True)
+    _check(grad_tokens, "grad_tokens", torch.bfloat16, numel=desc.M * desc.D, optional=True)
+    _check(grad_weight, "grad_weight", torch.bfloat16, numel=desc.V * desc.D, optional=True)
+    _check(grad_bias, "grad_bias", torch.float32, numel=desc.V, optional=True)
+    _check(workspace, "workspace", optional=True)
+    _one_device(loss, row_loss, grad_tokens, grad_weight, grad_bias, workspace, *desc.tensors,
+                stream=stream)
+    rc = load().mae_class_loss(C.byref(desc), _ptr(loss), _ptr(row_loss), _ptr(grad_tokens),
+                               _ptr(grad_weight), _ptr(grad_bias), _ptr(workspace),
+                               _bytes_of(workspace), _stream(stream))
+    if rc != MAE_OK:
+        raise MaeError(rc, "mae_class_loss")
 
 
 # ------------------------------------------------------------------------------------------------

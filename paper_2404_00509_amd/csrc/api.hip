@@ -9,14 +9,17 @@
 
 #include <atomic>
 
+#include "api_common.hpp"
 #include "mae_device.hpp"
 #include "mae_kernels.hpp"
 
 namespace {
 
-constexpr int kVersion = 600;  // 0.6.0
+using mae::aligned;
+using mae::have_device;
+using mae::validate_embed;
 
-bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+constexpr int kVersion = 700;  // 0.7.0
 
 struct PrepShape {
   int32_t G, L, D;
@@ -88,33 +91,6 @@ int validate_loss(const mae_loss_desc* d, bool need_target = true) {
   if (d->pred_dtype != MAE_F32 && d->pred_dtype != MAE_BF16) return MAE_ERR_DTYPE;
   if (d->norm_pix != 0 && d->norm_pix != 1) return MAE_ERR_RANGE;
   return MAE_OK;
-}
-
-int validate_embed(const mae_embed_desc* d) {
-  if (!d) return MAE_ERR_NULL;
-  if (!d->visible || !d->weight) return MAE_ERR_NULL;
-  if (d->pos && !d->ids_keep) return MAE_ERR_NULL;
-  if (d->M <= 0 || d->D <= 0 || d->E <= 0 || d->L <= 0) return MAE_ERR_SHAPE;
-  if (d->D % 4 != 0) return MAE_ERR_SHAPE;
-  if (d->M > (int64_t(1) << 28) || d->D > 3072 || d->E > 8192) return MAE_ERR_RANGE;
-  if (d->out_dtype != MAE_F32 && d->out_dtype != MAE_BF16) return MAE_ERR_DTYPE;
-  if (!aligned(d->visible, 16) || !aligned(d->weight, 16) || (d->pos && !aligned(d->pos, 16)))
-    return MAE_ERR_RANGE;
-  return MAE_OK;
-}
-
-// Whether this process sees a HIP device; asked once (the answer does not change while the
-// process lives) so that the launch paths do not query the runtime on every call.
-int have_device() {
-  static const int status = [] {
-    int n = 0;
-    if (hipGetDeviceCount(&n) != hipSuccess || n <= 0) {
-      (void)hipGetLastError();  // do not leave a sticky error for the caller's next HIP call
-      return (int)MAE_ERR_NO_DEVICE;
-    }
-    return (int)MAE_OK;
-  }();
-  return status;
 }
 
 }  // namespace

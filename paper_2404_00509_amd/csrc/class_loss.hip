@@ -1,0 +1,698 @@
+// Softmax cross entropy of a linear head over many classes (the finetuning recipe's loss, Sec. 3, Sec. 5.2, with
+// its label smoothing), with the gradients of tokens, weight and bias, and without ever
+// holding the logits: they are made on the matrix cores tile by tile, reduced, and made again where the gradient needs
+// them.
+//
+//   l = x W^T + b;  loss_n = lse(l_n) - (1 - s) l_n,y - s mean(l_n);  loss = mean of loss_n
+//   g = (softmax(l) - (1 - s) onehot(y) - s / V) grad_scale / count
+//   grad_x = g W, grad_W = g^T x, grad_b = sum over rows of g
+//
+//   pack    rows whose label is no class are left out: the others' numbers, labels and tokens one after the
+//           other, and their count, which the later kernels read from memory.  What such a row holds (NaN, infinities)
+//           touches nothing.  For the gradient also the largest magnitudes among tokens and weight
+//   stats   tiles of logits -> per row and tile the maximum, the sum of exponentials under it, the sum of logits
+//           (smoothing) and the label's logit
+//   rows    the tiles of a row joined -> maximum, 1 / sum, the row's loss
+//   halves  tokens and weight as fp16
+//   grad    tiles of logits again -> g as fp16 [rows, classes of the piece], sums of its columns in fp32
+//   matmul  g W (g along k, W across k) and g^T x (both across k); few tiles: k is split
+//   finish  the parts of a split joined, scaled, rounded once to bf16
+//
+// The gradient goes through the vocabulary in pieces, so g takes M x piece values of the workspace.
+// Logits are made as W x^T: a lane then holds up to 64 classes of one row, and the
+// reductions over classes stay in registers up to the last two steps.
+//
+// Types.  Logits: products of the bf16 operands, fp32 sums.  Maxima, exponentials and their sums: fp32; sums over rows of
+// the loss: double precision.  g, an operand of two products, is fp16 and not bf16: |g| <= 1, so that as 2^15 g it
+// loses at most 2^-11 of a value down to 2^-29, an eighth of what bf16 would, and less than the bf16 outputs
+// do by their own rounding (with bf16 a gradient of few rows and classes was up to 2.5 times as far from the exact one as
+// a result that is rounded once).  The other operand has to be fp16 too: scaled by the power of two that puts its largest value just
+// under 2^15, a bf16 number down to 2^-32 of that is exact.
+#include "mae_device.hpp"
+#include "mae_kernels.hpp"
+#include "matmul.hpp"
+
+namespace mae {
+
+namespace {
+
+using namespace mm;
+
+typedef f32x4 f32x4_a4 __attribute__((aligned(4)));
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kNegInf = -__builtin_inff();
+
+// exp(v) for v <= 0
+__device__ inline float exp_neg(float v) { return __builtin_amdgcn_exp2f(v * kLog2e); }
+
+// ---- pack -----------------------------------------------------------------------------------------
+constexpr int kPackThreads = 256;
+
+// The larger of `peak` and the finite magnitudes among eight bf16 values, as bits.
+__device__ inline int32_t peak_of(int32_t peak, u32x4 v) {
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const int32_t lo = v[k] & 0x7FFF, hi = (v[k] >> 16) & 0x7FFF;
+    if (lo < 0x7F80) peak = max(peak, lo);
+    if (hi < 0x7F80) peak = max(peak, hi);
+  }
+  return peak;
+}
+// The workgroup's largest to memory.
+__device__ inline void leave_peak(int32_t peak, int32_t* slots, int32_t* out) {
+#pragma unroll
+  for (int off = kWave / 2; off > 0; off >>= 1) peak = max(peak, __shfl_xor(peak, off, kWave));
+  __syncthreads();
+  if (threadIdx.x % kWave == 0) slots[threadIdx.x / kWave] = peak;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int w = 1; w < kPackThreads / kWave; ++w) peak = max(peak, slots[w]);
+    *out = peak;
+  }
+}
+// The factor that brings values of which `peak` is the largest under 2^15, as an exponent of two: fp16 holds
+// 2^15 times what is under 2.  At most 2^126 and at least 2^-113, so that it is a float and so is its inverse.
+__device__ inline int half_exponent(int32_t peak) {
+  const int e = (peak >> 7) - 127;  // 2^e <= the largest value < 2^(e + 1)
+  return min(14 - e, 126);
+}
+// largest of the peaks [from, to), by all lanes of a wavefront
+__device__ inline int32_t peak_among(const int32_t* peaks, int from, int to) {
+  int32_t p = 0;
+  for (int i = from + (int)(threadIdx.x % kWave); i < to; i += kWave) p = max(p, peaks[i]);
+#pragma unroll
+  for (int off = kWave / 2; off > 0; off >>= 1) p = max(p, __shfl_xor(p, off, kWave));
+  return p;
+}
+
+// Workgroups from pack_blocks on look for the largest magnitude of the weight.
+__global__ __launch_bounds__(kPackThreads) void class_pack_kernel(ClassArgs a) {
+  __shared__ int32_t wave_sum[kPackThreads / kWave];
+  __shared__ int32_t map[kPackThreads];
+  const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
+  int32_t peak = 0;
+  if ((int)blockIdx.x >= a.pack_blocks) {
+    const u32x4* w = reinterpret_cast<const u32x4*>(a.weight);
+    const int64_t n = (int64_t)a.V * a.D / 8;
+    for (int64_t i = (int64_t)((int)blockIdx.x - a.pack_blocks) * kPackThreads + tid; i < n;
+         i += (int64_t)(a.num_peaks - a.pack_blocks) * kPackThreads)
+      peak = peak_of(peak, w[i]);
+    leave_peak(peak, wave_sum, a.peaks + blockIdx.x);
+    return;
+  }
+  const int64_t row0 = (int64_t)blockIdx.x * a.pack_rows;
+  const int64_t end = min(row0 + a.pack_rows, a.M);
+  auto is_class = [&](int64_t r) { return (uint32_t)a.labels[r] < (uint32_t)a.V; };
+  // rows in front of this workgroup's that take part
+  int32_t before = 0;
+  for (int64_t r = tid; r < row0; r += kPackThreads) before += is_class(r) ? 1 : 0;
+#pragma unroll
+  for (int off = kWave / 2; off > 0; off >>= 1) before += __shfl_xor(before, off, kWave);
+  if (lane == 0) wave_sum[wave] = before;
+  __syncthreads();
+  int32_t at = 0;
+  for (int w = 0; w < kPackThreads / kWave; ++w) at += wave_sum[w];
+  for (int64_t base = row0; base < end; base += kPackThreads) {
+    const int64_t r = base + tid;
+    const bool in = r < end && is_class(r);
+    const uint64_t votes = __ballot(in);
+    __syncthreads();
+    if (lane == 0) wave_sum[wave] = __popcll(votes);
+    __syncthreads();
+    int32_t slot = at + __popcll(votes & ((1ull << lane) - 1));
+    for (int w = 0; w < wave; ++w) slot += wave_sum[w];
+    for (int w = 0; w < kPackThreads / kWave; ++w) at += wave_sum[w];
+    if (r < end) a.slot_of[r] = in ? slot : -1;
+    if (in) a.label_of[slot] = a.labels[r];
+    map[tid] = in ? slot : -1;
+    __syncthreads();
+    // the tokens, a wavefront per row, 16 bytes per lane
+    const int rows = (int)min((int64_t)kPackThreads, end - base);
+    for (int i = wave; i < rows; i += kPackThreads / kWave) {
+      const int32_t to = map[i];
+      if (to < 0) continue;
+      const u32x4* src = reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(a.tokens) + (base + i) * a.D);
+      u32x4* dst = reinterpret_cast<u32x4*>(a.packed + (int64_t)to * a.D);
+      for (int c = lane; c < a.D / 8; c += kWave) {
+        const u32x4 v = src[c];
+        if (a.peaks) peak = peak_of(peak, v);
+        dst[c] = v;
+      }
+    }
+  }
+  if (end == a.M && tid == 0) *a.count = at;
+  if (a.peaks) leave_peak(peak, wave_sum, a.peaks + blockIdx.x);
+}
+
+// ---- halves: eight values per lane -----------------------------------------------------------------
+__device__ inline uint32_t half_pair(float lo, float hi) {
+  typedef float in2 __attribute__((ext_vector_type(2)));
+  typedef _Float16 out2 __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector((in2{lo, hi}), out2));
+}
+__global__ __launch_bounds__(kPackThreads) void class_halves_kernel(ClassArgs a) {
+  const int64_t of_tokens = (int64_t)*a.count * (a.D / 8), of_weight = (int64_t)a.V * (a.D / 8);
+  const float ft = ldexpf(1.0f, half_exponent(peak_among(a.peaks, 0, a.pack_blocks)));
+  const float fw = ldexpf(1.0f, half_exponent(peak_among(a.peaks, a.pack_blocks, a.num_peaks)));
+  for (int64_t i = (int64_t)blockIdx.x * kPackThreads + threadIdx.x; i < of_tokens + of_weight;
+       i += (int64_t)gridDim.x * kPackThreads) {
+    const bool t = i < of_tokens;
+    const int64_t at = t ? i : i - of_tokens;
+    const u32x4 v = t ? reinterpret_cast<const u32x4*>(a.packed)[at] : reinterpret_cast<const u32x4*>(a.weight)[at];
+    const float f = t ? ft : fw;
+    u32x4 out;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) out[k] = half_pair(bf16_lo(v[k]) * f, bf16_hi(v[k]) * f);
+    reinterpret_cast<u32x4*>(t ? a.half_tokens : a.half_weight)[at] = out;
+  }
+}
+
+// ---- tiles of logits --------------------------------------------------------------------------------
+// acc[i][j][e]: class 32 (wm TM + i) + 8 (e / 4) + 4 (lane / 32) + e % 4 of the tile, row 32 (wn TN + j) + lane % 32.
+template <int TM, int TN>
+__device__ inline void add_bias(const float* bias, int first, int V, int lane, f32x16 (&acc)[TM][TN]) {
+  if (!bias) return;
+#pragma unroll
+  for (int i = 0; i < TM; ++i)
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int v = first + 32 * i + 8 * q + 4 * (lane >> 5);
+      f32x4 b = f32x4{0.f, 0.f, 0.f, 0.f};
+      if (v + 4 <= V) {
+        b = *reinterpret_cast<const f32x4_a4*>(bias + v);
+      } else {
+#pragma unroll
+        for (int k = 0; k < 3; ++k)
+          if (v + k < V) b[k] = bias[v + k];
+      }
+#pragma unroll
+      for (int j = 0; j < TN; ++j)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) acc[i][j][4 * q + k] += b[k];
+    }
+}
+
+template <class T>
+__device__ inline void logits_tile(const ClassArgs& a, int64_t v0, int64_t n0, int rows_v, int rows_n, u32x4* lds,
+                                   f32x16 (&acc)[T::BM / 32 / T::kWavesM][T::BN / 32 / T::kWavesN]) {
+  const Operand W{static_cast<const uint16_t*>(a.weight) + v0 * a.D, a.D, rows_v};
+  const Operand X{a.packed + n0 * a.D, a.D, rows_n};
+  T::run(W, X, a.D, lds, acc);
+}
+
+template <int TM, int TN, int WGM, int WGN, int STAGES>
+struct Logits : Tile<TM, TN, WGM, WGN, STAGES, true, true> {
+  static constexpr int kWavesM = WGM, kWavesN = WGN;
+};
+
+template <int TM, int TN, int WGM, int WGN, int STAGES>
+__global__ __launch_bounds__(64 * WGM * WGN) void class_stats_kernel(ClassArgs a) {
+  using T = Logits<TM, TN, WGM, WGN, STAGES>;
+  __shared__ __attribute__((aligned(1024))) u32x4 lds[T::kLdsBytes / 16];
+  const int count = uniform(*a.count);
+  const uint32_t tiles_v = (uint32_t)((a.V + T::BM - 1) / T::BM);
+  const uint32_t tile = xcd_remap(blockIdx.x, gridDim.x);
+  const uint32_t tn = tile / tiles_v, tv = tile - tn * tiles_v;
+  const int64_t n0 = (int64_t)tn * T::BN;
+  const int v0 = (int)tv * T::BM;
+  if (n0 >= count) return;
+  const int rows_n = (int)min((int64_t)T::BN, count - n0), rows_v = min(T::BM, a.V - v0);
+  const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
+  const int wm = wave / WGN, wn = wave % WGN;
+  f32x16 acc[TM][TN];
+  logits_tile<T>(a, v0, n0, rows_v, rows_n, lds, acc);
+  const int first = v0 + wm * 32 * TM;
+  add_bias<TM, TN>(a.bias, first, a.V, lane, acc);
+
+  __syncthreads();  // every wavefront is done with the staged operands
+  float* part = reinterpret_cast<float*>(lds);  // [WGM][BN][3]
+#pragma unroll
+  for (int j = 0; j < TN; ++j) {
+    const int r = wn * 32 * TN + j * 32 + (lane & 31);
+    const int y = r < rows_n ? a.label_of[n0 + r] - first - 4 * (lane >> 5) : -1;
+    float m = kNegInf, sl = 0.f, own = 0.f;
+    bool has = false;
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const int c = 32 * i + 8 * (e >> 2) + (e & 3);
+        const float l = acc[i][j][e];
+        if (c == y) {
+          own = l;
+          has = true;
+        }
+        const bool in = first + 4 * (lane >> 5) + c < a.V;
+        m = in ? fmaxf(m, l) : m;
+        if (in) sl += l;
+      }
+    m = fmaxf(m, __shfl_xor(m, 32, kWave));
+    float s = 0.f;
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const int c = 32 * i + 8 * (e >> 2) + (e & 3);
+        const bool in = first + 4 * (lane >> 5) + c < a.V;
+        // (a NaN among the logits reaches the sum; a tile of -inf only adds nothing)
+        const float x = m == kNegInf && acc[i][j][e] == kNegInf ? 0.f : exp_neg(acc[i][j][e] - m);
+        if (in) s += x;
+      }
+    s += __shfl_xor(s, 32, kWave);
+    sl += __shfl_xor(sl, 32, kWave);
+    if (has) a.label_logit[n0 + r] = own;
+    if (lane < 32) {
+      float* p = part + (wm * T::BN + r) * 3;
+      p[0] = m;
+      p[1] = s;
+      p[2] = sl;
+    }
+  }
+  __syncthreads();
+  for (int r = tid; r < rows_n; r += T::kThreads) {
+    float m = kNegInf, s = 0.f, sl = 0.f;
+#pragma unroll
+    for (int w = 0; w < WGM; ++w) m = fmaxf(m, part[(w * T::BN + r) * 3]);
+#pragma unroll
+    for (int w = 0; w < WGM; ++w) {
+      const float* p = part + (w * T::BN + r) * 3;
+      s += p[0] == kNegInf ? p[1] : p[1] * exp_neg(p[0] - m);
+      sl += p[2];
+    }
+    float* out = a.stats + ((n0 + r) * (int64_t)tiles_v + tv) * 2;
+    *reinterpret_cast<f32x2*>(out) = f32x2{m, s};
+    if (a.logit_sums) a.logit_sums[(n0 + r) * (int64_t)tiles_v + tv] = sl;
+  }
+}
+
+// ---- rows: a wavefront each --------------------------------------------------------------------------
+constexpr int kRowThreads = 256;
+__global__ __launch_bounds__(kRowThreads) void class_rows_kernel(ClassArgs a) {
+  __shared__ double sums[kRowThreads / kWave];
+  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+  const int64_t row = (int64_t)blockIdx.x * (kRowThreads / kWave) + wave;
+  double loss = 0.0;
+  if (row < a.M) {
+    const int slot = a.slot_of[row];
+    if (slot >= 0) {
+      const f32x2* st = reinterpret_cast<const f32x2*>(a.stats) + (int64_t)slot * a.stat_tiles;
+      float m = kNegInf, s = 0.f, sl = 0.f;
+      for (int t = lane; t < a.stat_tiles; t += kWave) m = fmaxf(m, st[t].x);
+#pragma unroll
+      for (int off = kWave / 2; off > 0; off >>= 1) m = fmaxf(m, __shfl_xor(m, off, kWave));
+      for (int t = lane; t < a.stat_tiles; t += kWave) {
+        const f32x2 p = st[t];
+        s += p.x == kNegInf ? p.y : p.y * exp_neg(p.x - m);
+        if (a.logit_sums) sl += a.logit_sums[(int64_t)slot * a.stat_tiles + t];
+      }
+#pragma unroll
+      for (int off = kWave / 2; off > 0; off >>= 1) {
+        s += __shfl_xor(s, off, kWave);
+        sl += __shfl_xor(sl, off, kWave);
+      }
+      float v = (m + logf(s)) - (1.0f - a.smoothing) * a.label_logit[slot];
+      if (a.logit_sums) v -= a.smoothing * (sl / (float)a.V);
+      loss = (double)v;
+      if (lane == 0) {
+        a.row_max[slot] = m;
+        a.row_inv[slot] = 1.0f / s;
+      }
+    }
+    if (lane == 0 && a.row_loss) a.row_loss[row] = (float)loss;
+  }
+  if (lane == 0) sums[wave] = loss;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    double s = 0.0;
+    for (int w = 0; w < kRowThreads / kWave; ++w) s += sums[w];
+    a.partials[blockIdx.x] = s;
+  }
+}
+
+// ---- the gradient of the logits, one piece of the classes -------------------------------------------------
+constexpr float kGScale = 32768.0f;  // of g as fp16
+
+// One step of adding kCount values over the 32 lanes of half a wavefront: lanes whose bit kMask is set go on
+// with the upper half of the values, the others with the lower half.
+template <int kCount, int kMask>
+__device__ inline void halve(float* v, int lane) {
+  if constexpr (kCount > 1) {
+#pragma unroll
+    for (int k = 0; k < kCount / 2; ++k) {
+      const bool up = (lane & kMask) != 0;
+      const float send = up ? v[k] : v[k + kCount / 2];
+      const float keep = up ? v[k + kCount / 2] : v[k];
+      v[k] = keep + __shfl_xor(send, kMask, kWave);
+    }
+  } else {
+    v[0] += __shfl_xor(v[0], kMask, kWave);
+  }
+}
+
+template <int TM, int TN, int WGM, int WGN, int STAGES>
+__global__ __launch_bounds__(64 * WGM * WGN) void class_grad_kernel(ClassArgs a) {
+  using T = Logits<TM, TN, WGM, WGN, STAGES>;
+  constexpr int kPitch = 32 * TM + 8;  // of a wavefront's strip of 32 rows, in fp16
+  constexpr int kStripBytes = WGM * WGN * 32 * kPitch * 2;
+  constexpr int kColBytes = WGN * T::BM * 4;
+  constexpr int kBytes = T::kLdsBytes > kStripBytes + kColBytes ? T::kLdsBytes : kStripBytes + kColBytes;
+  __shared__ __attribute__((aligned(1024))) u32x4 lds[kBytes / 16];
+  const int count = uniform(*a.count);
+  const uint32_t tiles_v = (uint32_t)((a.piece_classes + T::BM - 1) / T::BM);
+  const uint32_t tile = xcd_remap(blockIdx.x, gridDim.x);
+  const uint32_t tn = tile / tiles_v, tv = tile - tn * tiles_v;
+  const int64_t n0 = (int64_t)tn * T::BN;
+  const int c0 = (int)tv * T::BM;  // of the piece
+  const int v0 = a.piece_first + c0;
+  if (n0 >= count) return;
+  const int rows_n = (int)min((int64_t)T::BN, count - n0), rows_v = min(T::BM, a.piece_classes - c0);
+  const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
+  const int wm = wave / WGN, wn = wave % WGN;
+  f32x16 acc[TM][TN];
+  logits_tile<T>(a, v0, n0, rows_v, rows_n, lds, acc);
+  const int first = v0 + wm * 32 * TM;
+  add_bias<TM, TN>(a.bias, first, a.V, lane, acc);
+
+  __syncthreads();
+  uint16_t* strip = reinterpret_cast<uint16_t*>(lds) + wave * 32 * kPitch;
+  float* columns = reinterpret_cast<float*>(reinterpret_cast<char*>(lds) + kStripBytes);
+  const float uniform = a.smoothing / (float)a.V;
+  const int end = a.piece_first + a.piece_classes;  // classes of the piece
+  const int half = 4 * (lane >> 5);
+#pragma unroll
+  for (int j = 0; j < TN; ++j) {
+    const int r = wn * 32 * TN + j * 32 + (lane & 31);
+    const bool live = r < rows_n;
+    const float m = live ? a.row_max[n0 + r] : 0.f, inv = live ? a.row_inv[n0 + r] : 0.f;
+    const int y = live ? a.label_of[n0 + r] - first - half : -1;
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        float g[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const int c = 32 * i + 8 * q + k;
+          float v = exp_neg(acc[i][j][4 * q + k] - m) * inv - uniform;
+          if (c == y) v -= 1.0f - a.smoothing;
+          if (!live || first + half + c >= end) v = 0.f;
+          acc[i][j][4 * q + k] = v;
+          g[k] = v;
+        }
+        *reinterpret_cast<u32x2*>(strip + (lane & 31) * kPitch + 32 * i + 8 * q + half) =
+            u32x2{half_pair(g[0] * kGScale, g[1] * kGScale), half_pair(g[2] * kGScale, g[3] * kGScale)};
+      }
+    __builtin_amdgcn_wave_barrier();
+    // rows of the strip to memory, 16 bytes per lane
+    constexpr int kLanesPerRow = 4 * TM;
+    constexpr int kRowsPerRep = kWave / kLanesPerRow;
+#pragma unroll
+    for (int rep = 0; rep < 32 / kRowsPerRep; ++rep) {
+      const int sr = rep * kRowsPerRep + lane / kLanesPerRow;
+      const int col = (lane % kLanesPerRow) * 8;
+      const u32x4 v = *reinterpret_cast<const u32x4*>(strip + sr * kPitch + col);
+      const int row = wn * 32 * TN + j * 32 + sr;
+      const int c = c0 + wm * 32 * TM + col;
+      if (row < rows_n && c < a.piece_ld)
+        *reinterpret_cast<u32x4*>(a.g + (n0 + row) * (int64_t)a.piece_ld + c) = v;
+    }
+    __builtin_amdgcn_wave_barrier();
+  }
+  if (!a.column_sums) return;
+  // sums over the tile's rows: over j in registers, over 32 lanes by halving, over wavefronts through LDS
+  float v[16 * TM];
+#pragma unroll
+  for (int i = 0; i < TM; ++i)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      float s = acc[i][0][e];
+#pragma unroll
+      for (int j = 1; j < TN; ++j) s += acc[i][j][e];
+      v[16 * i + e] = s;
+    }
+  constexpr int N = 16 * TM;
+  halve<N, 16>(v, lane);
+  halve<(N > 1 ? N / 2 : 1), 8>(v, lane);
+  halve<(N > 2 ? N / 4 : 1), 4>(v, lane);
+  halve<(N > 4 ? N / 8 : 1), 2>(v, lane);
+  halve<(N > 8 ? N / 16 : 1), 1>(v, lane);
+  // the index of what is left: the lane's bits from the top down, then k
+  constexpr int kLeft = N >= 32 ? N / 32 : 1;
+  int base = 0;
+  {
+    int n = N;
+#pragma unroll
+    for (int mask = 16; mask > 0; mask >>= 1)
+      if (n > 1) {
+        n >>= 1;
+        if (lane & mask) base += n;
+      }
+  }
+#pragma unroll
+  for (int k = 0; k < kLeft; ++k) {
+    const int at = base + k, i = at >> 4, e = at & 15;
+    const int c = wm * 32 * TM + 32 * i + 8 * (e >> 2) + half + (e & 3);
+    columns[wn * T::BM + c] = v[k];  // (lanes that hold the same sum write the same value)
+  }
+  __syncthreads();
+  for (int c = tid; c < rows_v; c += T::kThreads) {
+    float s = columns[c];
+#pragma unroll
+    for (int w = 1; w < WGN; ++w) s += columns[w * T::BM + c];
+    a.column_sums[(int64_t)tn * a.piece_classes + c0 + c] = s;
+  }
+}
+
+// ---- finish -----------------------------------------------------------------------------------------
+__device__ inline double grad_factor(const ClassArgs& a) {
+  const int n = *a.count;
+  return n > 0 ? (double)a.grad_scale / (double)n : 0.0;
+}
+// A product's sum to a gradient, with the powers of two of its operands taken out: `rest` is the factor of the
+// operand beside g.  (That factor may be as far from 1 as floats go, so it is not multiplied into `factor`.)
+struct Scale {
+  float factor;
+  int rest;
+  __device__ inline float operator()(float v) const { return ldexpf(v * factor, rest); }
+};
+__device__ inline Scale product_scale(const ClassArgs& a, int from, int to) {
+  return Scale{(float)(grad_factor(a) / (double)kGScale), -half_exponent(peak_among(a.peaks, from, to))};
+}
+__device__ inline u32x4 pack8(const float (&v)[8]) {
+  return u32x4{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])};
+}
+// eight values at `at` of the first of `parts` arrays that lie `stride` values apart, added up
+__device__ inline void sum_parts(const float* p, int64_t at, int64_t stride, int parts, float (&v)[8]) {
+#pragma unroll
+  for (int k = 0; k < 8; ++k) v[k] = 0.f;
+  for (int s = 0; s < parts; ++s) {
+    const f32x4 lo = *reinterpret_cast<const f32x4*>(p + s * stride + at);
+    const f32x4 hi = *reinterpret_cast<const f32x4*>(p + s * stride + at + 4);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      v[k] += lo[k];
+      v[4 + k] += hi[k];
+    }
+  }
+}
+
+constexpr int kFinishThreads = 256;
+// grad_tokens: eight values per lane
+__global__ __launch_bounds__(kFinishThreads) void class_tokens_kernel(ClassArgs a) {
+  const int per_row = a.D / 8;
+  const Scale scaled = product_scale(a, a.pack_blocks, a.num_peaks);
+  const int64_t total = a.M * per_row;
+  for (int64_t i = (int64_t)blockIdx.x * kFinishThreads + threadIdx.x; i < total;
+       i += (int64_t)gridDim.x * kFinishThreads) {
+    const int64_t row = i / per_row;
+    const int c = (int)(i - row * per_row) * 8;
+    const int slot = a.slot_of[row];
+    float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    if (slot >= 0) {
+      sum_parts(a.tokens_acc, (int64_t)slot * a.D + c, a.M * a.D, a.tokens_parts, v);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[k] = scaled(v[k]);
+    }
+    *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(a.grad_tokens) + row * a.D + c) = pack8(v);
+  }
+}
+
+// grad_weight of the piece
+__global__ __launch_bounds__(kFinishThreads) void class_weight_kernel(ClassArgs a) {
+  const Scale scaled = product_scale(a, 0, a.pack_blocks);
+  const int64_t stride = (int64_t)a.piece_classes * a.D, total = stride / 8;
+  for (int64_t i = (int64_t)blockIdx.x * kFinishThreads + threadIdx.x; i < total;
+       i += (int64_t)gridDim.x * kFinishThreads) {
+    float v[8];
+    sum_parts(a.weight_acc, i * 8, stride, a.weight_parts, v);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = scaled(v[k]);
+    *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(a.grad_weight) + (int64_t)a.piece_first * a.D + i * 8) = pack8(v);
+  }
+}
+
+// grad_bias of the piece: 64 classes by 4 lanes each
+__global__ __launch_bounds__(kFinishThreads) void class_bias_kernel(ClassArgs a) {
+  __shared__ float part[4][64];
+  const int col = threadIdx.x % 64, r = threadIdx.x / 64;
+  const int c = blockIdx.x * 64 + col;
+  const int tiles = (*a.count + a.grad_rows - 1) / a.grad_rows;
+  float s = 0.f;
+  if (c < a.piece_classes)
+    for (int t = r; t < tiles; t += 4) s += a.column_sums[(int64_t)t * a.piece_classes + c];
+  part[r][col] = s;
+  __syncthreads();
+  if (r == 0 && c < a.piece_classes)
+    a.grad_bias[a.piece_first + c] = ((part[0][col] + part[1][col]) + (part[2][col] + part[3][col])) * (float)grad_factor(a);
+}
+
+}  // namespace
+
+// ---- host ---------------------------------------------------------------------------------------------
+namespace {
+
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+size_t up256(size_t n) { return (n + 255) & ~size_t(255); }
+
+// Side of the tiles of logits.
+int logits_side(int64_t M, int V) {
+  if (ceil_div(M, 128) * ceil_div(V, 128) < 128) return 64;
+  if (ceil_div(M, 256) * ceil_div(V, 256) < 512) return 128;
+  return 256;
+}
+
+}  // namespace
+
+ClassPlan class_plan(int64_t M, int D, int V, bool grad) {
+  ClassPlan p{};
+  p.side = logits_side(M, V);
+  p.stat_tiles = (int)ceil_div(V, p.side);
+  p.pack_rows = (int)ceil_div(ceil_div(M, 1024), 64) * 64;
+  // g of a piece takes at most 512 MiB, or 1024 classes
+  const int64_t most = (int64_t(1) << 28) / M / 256 * 256;
+  p.piece = (int)(most < 1024 ? 1024 : most < V ? most : V);
+  if (p.piece > V) p.piece = V;
+  p.piece_ld = (int)ceil_div(p.piece, 64) * 64;
+  p.tokens_side = matmul_side(M, D);
+  p.tokens_parts = matmul_parts(M, D, p.piece, p.tokens_side);
+  p.weight_side = matmul_side(p.piece, D);
+  p.weight_parts = matmul_parts(p.piece, D, M, p.weight_side);
+  size_t at = 0;
+  const auto take = [&](size_t bytes) {
+    const size_t was = at;
+    at += up256(bytes);
+    return was;
+  };
+  const size_t m = (size_t)M;
+  p.count = take(sizeof(int32_t));
+  p.slot_of = take(m * 4);
+  p.label_of = take(m * 4);
+  p.packed = take(m * D * 2);
+  p.stats = take(m * p.stat_tiles * 8);
+  p.logit_sums = take(m * p.stat_tiles * 4);
+  p.label_logit = take(m * 4);
+  p.row_max = take(m * 4);
+  p.row_inv = take(m * 4);
+  p.num_partials = (int)ceil_div(M, kRowThreads / kWave);
+  p.partials = take((size_t)p.num_partials * 8);
+  if (grad) {
+    p.num_weight_peaks = (int)min(ceil_div((int64_t)V * D / 8, kPackThreads * 4), (int64_t)512);
+    p.num_peaks = (int)ceil_div(M, p.pack_rows) + p.num_weight_peaks;
+    p.peaks = take((size_t)p.num_peaks * 4);
+    p.half_tokens = take(m * D * 2);
+    p.half_weight = take((size_t)V * D * 2);
+    p.g = take(m * p.piece_ld * 2);
+    p.column_sums = take((size_t)ceil_div(M, p.side) * p.piece * 4);
+    p.tokens_acc = take(m * D * 4 * p.tokens_parts);
+    p.weight_acc = take((size_t)p.piece * D * 4 * p.weight_parts);
+  }
+  p.bytes = at;
+  return p;
+}
+
+namespace {
+template <int TM, int TN, int WGM, int WGN, int STAGES>
+void launch_stats(const ClassArgs& a, hipStream_t stream) {
+  using T = Logits<TM, TN, WGM, WGN, STAGES>;
+  const int64_t tiles = ceil_div(a.M, T::BN) * ceil_div(a.V, T::BM);
+  hipLaunchKernelGGL((class_stats_kernel<TM, TN, WGM, WGN, STAGES>), dim3((uint32_t)tiles), dim3(T::kThreads), 0,
+                     stream, a);
+}
+template <int TM, int TN, int WGM, int WGN, int STAGES>
+void launch_grad(const ClassArgs& a, hipStream_t stream) {
+  using T = Logits<TM, TN, WGM, WGN, STAGES>;
+  const int64_t tiles = ceil_div(a.M, T::BN) * ceil_div(a.piece_classes, T::BM);
+  hipLaunchKernelGGL((class_grad_kernel<TM, TN, WGM, WGN, STAGES>), dim3((uint32_t)tiles), dim3(T::kThreads), 0,
+                     stream, a);
+}
+uint32_t finish_blocks(int64_t values) {
+  const int64_t blocks = ceil_div(values / 8, kFinishThreads);
+  return (uint32_t)(blocks < 1 ? 1 : blocks < 65536 ? blocks : 65536);
+}
+}  // namespace
+
+hipError_t launch_class_loss(ClassArgs a, const ClassPlan& p, hipStream_t stream) {
+  a.pack_rows = p.pack_rows;
+  a.stat_tiles = p.stat_tiles;
+  a.pack_blocks = (int)ceil_div(a.M, p.pack_rows);
+  a.num_peaks = p.num_peaks;
+  hipLaunchKernelGGL(class_pack_kernel, dim3((uint32_t)(a.peaks ? p.num_peaks : a.pack_blocks)), dim3(kPackThreads), 0,
+                     stream, a);
+  if (p.side == 256) launch_stats<4, 2, 2, 4, 2>(a, stream);
+  else if (p.side == 128) launch_stats<2, 1, 2, 4, 2>(a, stream);
+  else launch_stats<1, 1, 2, 2, 3>(a, stream);
+  hipLaunchKernelGGL(class_rows_kernel, dim3((uint32_t)p.num_partials), dim3(kRowThreads), 0, stream, a);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  e = launch_loss_finish(a.partials, p.num_partials, 0.0, a.loss, a.count, 1, 1, stream);
+  if (e != hipSuccess) return e;
+  if (!a.grad_tokens && !a.grad_weight && !a.grad_bias) return hipSuccess;
+
+  hipLaunchKernelGGL(class_halves_kernel, dim3((uint32_t)min(ceil_div((a.M + a.V) * a.D / 8, kPackThreads), (int64_t)4096)),
+                     dim3(kPackThreads), 0, stream, a);
+  a.piece_ld = p.piece_ld;
+  a.grad_rows = p.side;
+  a.tokens_parts = p.tokens_parts;
+  a.weight_parts = p.weight_parts;
+  if (!a.grad_bias) a.column_sums = nullptr;
+  for (int first = 0; first < a.V; first += p.piece) {
+    a.piece_first = first;
+    a.piece_classes = a.V - first < p.piece ? a.V - first : p.piece;
+    if (p.side == 256) launch_grad<4, 2, 2, 4, 2>(a, stream);
+    else if (p.side == 128) launch_grad<2, 1, 2, 4, 2>(a, stream);
+    else launch_grad<1, 1, 2, 2, 3>(a, stream);
+    e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    const uint16_t* weight = a.half_weight + (int64_t)first * a.D;
+    if (a.grad_tokens) {
+      // rows: packed rows; k: classes of the piece (g holds zeros up to a multiple of 8 behind them)
+      MatmulArgs m{};
+      m.A = a.g, m.lda = p.piece_ld, m.B = weight, m.ldb = a.D;
+      m.M = a.M, m.N = a.D, m.K = a.piece_classes, m.rows = a.count;
+      m.out = a.tokens_acc, m.parts = p.tokens_parts, m.accumulate = first > 0;
+      e = launch_matmul(m, MatmulKind::kHalfAlong, p.tokens_side, stream);
+      if (e != hipSuccess) return e;
+    }
+    if (a.grad_weight) {
+      MatmulArgs m{};
+      m.A = a.g, m.lda = p.piece_ld, m.B = a.half_tokens, m.ldb = a.D;
+      m.M = a.piece_classes, m.N = a.D, m.K = a.M, m.depth = a.count;
+      m.out = a.weight_acc, m.parts = p.weight_parts;
+      e = launch_matmul(m, MatmulKind::kHalfAcross, p.weight_side, stream);
+      if (e != hipSuccess) return e;
+      hipLaunchKernelGGL(class_weight_kernel, dim3(finish_blocks((int64_t)a.piece_classes * a.D)),
+                         dim3(kFinishThreads), 0, stream, a);
+    }
+    if (a.grad_bias)
+      hipLaunchKernelGGL(class_bias_kernel, dim3((uint32_t)ceil_div(a.piece_classes, 64)), dim3(kFinishThreads), 0,
+                         stream, a);
+    e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  if (a.grad_tokens)
+    hipLaunchKernelGGL(class_tokens_kernel, dim3(finish_blocks(a.M * a.D)), dim3(kFinishThreads), 0, stream, a);
+  return hipGetLastError();
+}
+
+}  // namespace mae

@@ -236,4 +236,142 @@ struct EmbedArgs {
 int embed_tile(int64_t M, int D, int E);
 hipError_t launch_patch_embed(const EmbedArgs& a, hipStream_t stream);
 
+// ---- layer norm of token rows ------------------------------------------------------------------------
+struct NormArgs {
+  int64_t M;
+  int32_t D, padded;  // padded: D rounded up to 4
+  int32_t x_bf16, y_bf16;
+  float eps;
+  const void* x;
+  const float* weight;  // [D], nullable
+  const float* bias;    // [D], nullable
+  void* y;
+  float* mean_out;  // [M], nullable
+  float* rstd_out;  // [M], nullable
+  // backward
+  const void* grad_y;
+  const float* mean;
+  const float* rstd;
+  void* grad_x;        // nullable
+  float* partials;     // [num_partials][2][padded]; null: no gradient of weight and bias
+  int32_t num_partials;
+  float* grad_weight;  // nullable
+  float* grad_bias;    // nullable
+};
+int norm_partials(int64_t M, int D);  // workgroups of the backward kernel
+hipError_t launch_layer_norm(const NormArgs& a, hipStream_t stream);
+hipError_t launch_layer_norm_grad(const NormArgs& a, hipStream_t stream);
+
+// ---- dropout from the keyed draws --------------------------------------------------------------------
+struct DropoutArgs {
+  int64_t count;       // values
+  uint64_t key;        // of the call's draws
+  uint64_t threshold;  // a value is kept iff its 32 bits are not below
+  uint64_t first;      // index of value 0 (one draw per value), or its place in group `group0`
+  uint64_t span;       // 0: one draw per value; else values that share one
+  uint64_t group0;
+  float scale;         // 1 / (1 - p)
+  int32_t bf16;
+  const void* x;
+  const void* residual;  // nullable
+  void* y;
+};
+hipError_t launch_dropout(const DropoutArgs& a, hipStream_t stream);
+
+// ---- products of bf16 or fp16 matrices into fp32 parts -----------------------------------------------------------
+// part s of out[s][m][n] = sum over its share of k of A(m, k) B[k][n], B with k as its row number
+struct MatmulArgs {
+  const uint16_t* A;  // "along": A[m][k]; otherwise A[k][m]
+  const uint16_t* B;  // B[k][n]
+  int64_t lda, ldb;   // values from row to row
+  int64_t M, K;
+  int32_t N, parts;
+  const int32_t* rows;   // nullable: only so many m (device memory)
+  const int32_t* depth;  // nullable: only so many k
+  float* out;
+  int32_t accumulate;  // added to what is there
+};
+int matmul_side(int64_t M, int N);                             // of the tiles
+int matmul_parts(int64_t M, int N, int64_t K, int side);       // k is split into
+enum class MatmulKind { kHalfAlong, kHalfAcross, kBf16Across };  // operands' type, how A lies
+hipError_t launch_matmul(const MatmulArgs& a, MatmulKind kind, int side, hipStream_t stream);
+
+// ---- softmax cross entropy of a linear head ----------------------------------------------------------------
+struct ClassPlan {
+  int side;                       // of the tiles of logits
+  int stat_tiles, pack_rows, num_partials;
+  int piece, piece_ld;            // classes per piece of the gradient; row length of g
+  int tokens_side, tokens_parts;  // product for grad_tokens
+  int weight_side, weight_parts;  // product for grad_weight
+  // places in the workspace
+  size_t count, slot_of, label_of, packed, stats, logit_sums, label_logit, row_max, row_inv, partials;
+  int num_peaks, num_weight_peaks;  // workgroups of the first kernel; of them, those that look at the weight
+  size_t peaks, half_tokens, half_weight, g, column_sums, tokens_acc, weight_acc;
+  size_t bytes;
+};
+ClassPlan class_plan(int64_t M, int D, int V, bool grad);
+struct ClassArgs {
+  int64_t M;
+  int32_t D, V;
+  float smoothing, grad_scale;
+  const void* tokens;     // [M, D] bf16
+  const void* weight;     // [V, D] bf16
+  const float* bias;      // [V], nullable
+  const int32_t* labels;  // [M]
+  float* loss;
+  float* row_loss;    // [M], nullable
+  void* grad_tokens;  // [M, D] bf16, nullable
+  void* grad_weight;  // [V, D] bf16, nullable
+  float* grad_bias;   // [V], nullable
+  // workspace: rows whose label is a class, one after the other ("slots")
+  int32_t* count;      // their number
+  int32_t* slot_of;    // [M] slot of a row, -1: left out
+  int32_t* label_of;   // [slot]
+  uint16_t* packed;    // [slot][D]
+  float* stats;        // [slot][stat_tiles][2] maximum, sum of exponentials
+  float* logit_sums;   // [slot][stat_tiles], null without smoothing
+  float* label_logit;  // [slot]
+  float* row_max;      // [slot]
+  float* row_inv;      // [slot] 1 / sum of exponentials under the maximum
+  double* partials;
+  int32_t* peaks;         // [num_peaks] largest finite magnitudes as bf16 bits: tokens, then weight; null: no gradient
+  uint16_t* half_tokens;  // [slot][D] fp16, scaled by a power of two
+  uint16_t* half_weight;  // [V][D]
+  uint16_t* g;            // [slot][piece_ld] fp16, times 2^15
+  float* column_sums;  // [row tile][classes of the piece]
+  float* tokens_acc;   // [tokens_parts][M][D]
+  float* weight_acc;   // [weight_parts][classes of the piece][D]
+  // filled in by the launcher
+  int32_t pack_rows, stat_tiles, pack_blocks, num_peaks;
+  int32_t piece_first, piece_classes, piece_ld, grad_rows, tokens_parts, weight_parts;
+};
+hipError_t launch_class_loss(ClassArgs a, const ClassPlan& p, hipStream_t stream);
+
+// ---- gradients of the patch embedding --------------------------------------------------------------------
+struct EmbedGradPlan {
+  int ld;        // row length of g: E, or E rounded up to 8 in a copy
+  int last_row;  // the last row's products come from the joining kernel
+  int rows;      // rows of grad_pos that are summed (1: the bias alone)
+  int side, parts, chunk_rows, chunks, shares;
+  size_t padded, counts, starts, order, pos_parts, weight_acc, bytes;
+};
+EmbedGradPlan embed_grad_plan(int64_t M, int D, int E, int L, bool by_index);
+struct EmbedGradArgs {
+  int64_t M;
+  int32_t D, E, L;
+  const uint16_t* g;        // [M, E] bf16
+  const uint16_t* visible;  // [M, D] bf16
+  const int32_t* ids;       // [M]
+  float* grad_weight;       // [E, D], nullable
+  float* grad_bias;         // [E], nullable
+  float* grad_pos;          // [L, E], nullable
+  int32_t* counts;          // [chunks][L]
+  int32_t* starts;          // [L + 1]
+  int32_t* order;           // [M], null: no grad_pos, rows in their own order
+  float* pos_parts;         // [rows][shares][ld]
+  float* weight_acc;        // [parts][E][D]
+  int32_t ld, parts, shares, chunks, chunk_rows, last_row;
+};
+hipError_t launch_embed_grad(EmbedGradArgs a, const EmbedGradPlan& p, uint16_t* padded, hipStream_t stream);
+
 }  // namespace mae

@@ -1,0 +1,200 @@
+"""Gradients of the patch embedding.  With whole numbers as inputs every product and every sum below 2^24 is exact in
+fp32, so the results have to be equal to integer arithmetic; with random ones they are held to the bound of fp32
+sums."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2404_00509_amd as mae
+from paper_2404_00509_amd import synth
+from train_reference import U32, check
+
+pytestmark = pytest.mark.gpu
+
+BF16 = torch.bfloat16
+
+
+def _whole(seed, M, D, E, L, most=3):
+    g = torch.Generator(device="cuda").manual_seed(seed * 7919 + M + D + E)
+    r = lambda *s: torch.randint(-most, most + 1, s, generator=g, device="cuda").to(BF16)  # noqa: E731
+    return r(M, D), r(M, E), torch.randint(0, L, (M,), generator=g, device="cuda", dtype=torch.int32)
+
+
+def _desc(visible, ids, E, L):
+    w = torch.zeros(E, visible.shape[-1], dtype=BF16, device="cuda")  # not read
+    pos = None if ids is None else torch.zeros(L, E, device="cuda")
+    d = mae.make_embed_desc(visible, ids, w, None, pos)
+    return d, (w, pos)
+
+
+def _run(visible, g, ids, L, want=(True, True, True), stream=None):
+    E, D = g.shape[-1], visible.shape[-1]
+    desc, keep = _desc(visible, ids, E, L)
+    ws = torch.full((mae.mae_patch_embed_grad_workspace_bytes(desc),), 0xFF, dtype=torch.uint8, device="cuda")
+    out = [torch.full(s, float("nan"), device="cuda") if on else None
+           for on, s in zip(want, ((E, D), (E,), (L, E)))]
+    mae.mae_patch_embed_grad(desc, g, *out, ws, stream=stream)
+    torch.cuda.synchronize()
+    return out
+
+
+def _plain(visible, g, ids, L):
+    v, gd = visible.double(), g.double()
+    pos = torch.zeros(L, g.shape[-1], dtype=torch.float64, device="cuda")
+    if ids is not None:
+        pos.index_add_(0, ids.clamp(0, L - 1).long(), gd)
+    return gd.T.contiguous() @ v, gd.sum(0), pos
+
+
+# token rows, values per patch, width, patches: tiles of 64, 128 and 256, whole and ragged, one row, rows on 16-, 8-, 4-
+# and 2-byte boundaries, sums of less than a slice of 64, of several, of many
+SIZES = [(1, 4, 1, 1), (1, 8, 8, 4), (2, 12, 3, 5), (63, 48, 64, 16), (64, 64, 64, 16), (65, 192, 130, 49),
+         (700, 588, 1024, 256), (1000, 768, 768, 196), (3001, 768, 192, 196), (513, 100, 70, 49), (257, 36, 129, 16),
+         (5000, 972, 1000, 100), (333, 1200, 1004, 64), (20000, 48, 384, 9), (4097, 2700, 260, 7), (300, 64, 8192, 3)]
+
+
+@pytest.mark.parametrize("M,D,E,L", SIZES)
+def test_whole_numbers_are_exact(M, D, E, L):
+    visible, g, ids = _whole(1, M, D, E, L)
+    for got, want, name in zip(_run(visible, g, ids, L), _plain(visible, g, ids, L), ("weight", "bias", "pos")):
+        assert torch.equal(got.double(), want), name
+    weight, bias, _ = _run(visible, g, None, L, (True, True, False))
+    ref = _plain(visible, g, None, L)
+    assert torch.equal(weight.double(), ref[0]) and torch.equal(bias.double(), ref[1])
+
+
+def test_the_headline_batch():
+    M, D, E, L = 4096 * 49, 768, 768, 196
+    visible, g, _ = _whole(2, M, D, E, L, most=2)  # sums stay below 200704 * 4 < 2^24
+    ids = torch.rand(4096, L, device="cuda").argsort(1)[:, :49].to(torch.int32).contiguous().reshape(-1)
+    for got, want, name in zip(_run(visible, g, ids, L), _plain(visible, g, ids, L), ("weight", "bias", "pos")):
+        assert torch.equal(got.double(), want), name
+
+
+@pytest.mark.parametrize("M,D,E,L", [(2000, 588, 384, 256), (9000, 768, 768, 196)])
+def test_random_values(M, D, E, L):
+    g = torch.Generator(device="cuda").manual_seed(M)
+    visible = torch.randn(M, D, generator=g, device="cuda").to(BF16)
+    grad = (1e-3 * torch.randn(M, E, generator=g, device="cuda")).to(BF16)
+    ids = torch.randint(0, L, (M,), generator=g, device="cuda", dtype=torch.int32)
+    got, want = _run(visible, grad, ids, L), _plain(visible, grad, ids, L)
+    size = _plain(visible.abs(), grad.abs(), ids, L)
+    for a, b, s, name in zip(got, want, size, ("weight", "bias", "pos")):
+        check(a, b, (M + 2) * U32 * s, name)
+        # the typical error is that of a sum whose errors do not pile up
+        assert float(((a.double() - b).square().mean() / b.square().mean()).sqrt()) < 2e-6, name
+
+
+def test_indices_outside_the_grid_and_patches_without_tokens():
+    M, D, E, L = 500, 64, 96, 40
+    visible, g, ids = _whole(3, M, D, E, L)
+    wild = ids.clone()
+    wild[::3], wild[1::3] = -7, L + 1000
+    got, want = _run(visible, g, wild, L), _plain(visible, g, wild, L)
+    assert all(torch.equal(a.double(), b) for a, b in zip(got, want))
+    some = torch.where(ids % 2 == 0, ids, ids - 1)  # odd patches have no token
+    got = _run(visible, g, some, L)
+    assert not got[2][1::2].any() and torch.equal(got[2].double(), _plain(visible, g, some, L)[2])
+    one = torch.full_like(ids, 17)  # all tokens of one patch
+    got = _run(visible, g, one, L)
+    assert torch.equal(got[2].double(), _plain(visible, g, one, L)[2])
+
+
+def test_many_patch_indices():
+    M, D, E, L = 30000, 8, 40, 8192
+    visible, g, ids = _whole(4, M, D, E, L)
+    got, want = _run(visible, g, ids, L), _plain(visible, g, ids, L)
+    assert all(torch.equal(a.double(), b) for a, b in zip(got, want))
+
+
+@pytest.mark.parametrize("E", [384, 70])
+def test_each_output_by_itself_and_the_same_bits_again(E):
+    M, D, L = 3000, 588, 64
+    g = torch.Generator(device="cuda").manual_seed(5)
+    visible = torch.randn(M, D, generator=g, device="cuda").to(BF16)
+    grad = torch.randn(M, E, generator=g, device="cuda").to(BF16)
+    ids = torch.randint(0, L, (M,), generator=g, device="cuda", dtype=torch.int32)
+    whole = _run(visible, grad, ids, L)
+    for _ in range(2):
+        assert all(torch.equal(a, b) for a, b in zip(_run(visible, grad, ids, L), whole))
+    for k in (0, 2):
+        part = _run(visible, grad, ids, L, tuple(i == k for i in range(3)))
+        assert torch.equal(part[k], whole[k]), k
+    bias = _run(visible, grad, ids, L, (False, True, False))[1]
+    check(bias, grad.double().sum(0), M * U32 * grad.double().abs().sum(0), "bias alone")
+
+
+def test_values_behind_the_rows_are_not_used():
+    # the last row ends where the tensors end; what lies behind is NaN
+    for M, D, E in ((129, 588, 100), (64, 12, 4), (70, 36, 20)):
+        visible, g, ids = _whole(6, M, D, E, 5)
+        room_v = torch.full((M * D + 64,), float("nan"), dtype=BF16, device="cuda")
+        room_g = torch.full((M * E + 64,), float("nan"), dtype=BF16, device="cuda")
+        room_v[:M * D], room_g[:M * E] = visible.reshape(-1), g.reshape(-1)
+        got = _run(room_v[:M * D].view(M, D), room_g[:M * E].view(M, E), ids, 5)
+        for a, b in zip(got, _plain(visible, g, ids, 5)):
+            assert torch.equal(a.double(), b), (M, D, E)
+
+
+def test_gradient_against_differences_of_the_embedding():
+    # tokens are linear in weight, bias and pos: with whole numbers the difference is exact
+    M, D, E, L = 200, 64, 48, 25
+    visible, c, ids = _whole(7, M, D, E, L)
+    got = _run(visible, c, ids, L)
+    rng = np.random.default_rng(0)
+    w, dw = (torch.from_numpy(rng.integers(-2, 3, (E, D)).astype(np.float32)).cuda() for _ in range(2))
+    b, db = (torch.from_numpy(rng.integers(-2, 3, E).astype(np.float32)).cuda() for _ in range(2))
+    pos, dp = (torch.from_numpy(rng.integers(-2, 3, (L, E)).astype(np.float32)).cuda() for _ in range(2))
+
+    def value(w, b, pos):
+        tokens = torch.empty(M, E, device="cuda")
+        mae.mae_patch_embed(mae.make_embed_desc(visible, ids, w.to(BF16), b, pos, out_dtype=mae.MAE_F32), tokens)
+        return float((tokens.double() * c.double()).sum())
+
+    base = value(w, b, pos)
+    assert value(w + dw, b, pos) - base == float((got[0].double() * dw.double()).sum())
+    assert value(w, b + db, pos) - base == float((got[1].double() * db.double()).sum())
+    assert value(w, b, pos + dp) - base == float((got[2].double() * dp.double()).sum())
+
+
+def test_side_stream_and_replays_of_a_graph():
+    M, D, E, L = 2500, 768, 384, 196
+    visible, g, ids = _whole(8, M, D, E, L)
+    want = _run(visible, g, ids, L)
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        got = _run(visible, g, ids, L, stream=side)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    desc, keep = _desc(visible, ids, E, L)
+    ws = torch.empty(mae.mae_patch_embed_grad_workspace_bytes(desc), dtype=torch.uint8, device="cuda")
+    out = [torch.empty_like(t) for t in want]
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        mae.mae_patch_embed_grad(desc, g, *out, ws, stream=torch.cuda.current_stream())
+    for k in range(3):
+        for t in out:
+            t.fill_(float("nan"))
+        ws.fill_(0xFF)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(out, want)), k
+        visible.mul_(1.0)
+
+
+def test_after_the_input_pipeline():
+    wl = synth.WORKLOADS["c1"]
+    B, E = 16, 192
+    data = [torch.from_numpy(a).cuda() for a in synth.make_images(wl.kind, B, seed=5)]
+    K = mae.mae_num_keep(wl.L, wl.mask_ratio)
+    desc = mae.make_prep_desc(*data, out_size=wl.out_size, patch=wl.patch, num_keep=K, seed=3, batch_index=1,
+                              out_dtype=mae.MAE_BF16)
+    buf = mae.alloc_prep_buffers(desc)
+    mae.mae_prep_batch(desc, buf.visible, buf.mask, buf.ids_restore, buf.ids_keep, buf.target, buf.crop, buf.workspace)
+    g = torch.randn(B, K, E, device="cuda").to(BF16)
+    visible, ids = buf.visible.reshape(B * K, wl.D), buf.ids_keep.reshape(-1)
+    got = _run(visible, g.reshape(B * K, E), ids, wl.L)
+    want, size = _plain(visible, g.reshape(B * K, E), ids, wl.L), _plain(visible.abs(), g.reshape(B * K, E).abs(), ids, wl.L)
+    for a, b, s, name in zip(got, want, size, ("weight", "bias", "pos")):
+        check(a, b, (B * K + 2) * U32 * s, name)
