@@ -193,75 +193,109 @@ __device__ inline void add_bias(const float* bias, int first, int V, int lane, f
     }
 }
 
-template <class T>
-__device__ inline void logits_tile(const ClassArgs& a, int64_t v0, int64_t n0, int rows_v, int rows_n, u32x4* lds,
-                                   f32x16 (&acc)[T::BM / 32 / T::kWavesM][T::BN / 32 / T::kWavesN]) {
-  const Operand W{static_cast<const uint16_t*>(a.weight) + v0 * a.D, a.D, rows_v};
-  const Operand X{a.packed + n0 * a.D, a.D, rows_n};
-  T::run(W, X, a.D, lds, acc);
-}
+template <int TM, int TN, int WGM, int WGN>
+struct Logits : Tile<TM, TN, WGM, WGN, true, true> {
+  using Base = Tile<TM, TN, WGM, WGN, true, true>;
 
-template <int TM, int TN, int WGM, int WGN, int STAGES>
-struct Logits : Tile<TM, TN, WGM, WGN, STAGES, true, true> {
-  static constexpr int kWavesM = WGM, kWavesN = WGN;
+  // Where tile number `id` lies; classes [first, first + classes).
+  struct Place {
+    int tv, tn;          // column and row of the grid of tiles
+    int c0;              // first class, counted from `first`
+    int64_t n0;          // first row
+    int rows_v, rows_n;  // that exist
+    typename Base::Source source;
+  };
+  __device__ static inline Place place(const ClassArgs& a, uint32_t id, uint32_t tiles, int count, int first, int classes) {
+    const uint32_t tiles_v = (uint32_t)((classes + Base::BM - 1) / Base::BM);
+    uint32_t tn, tv;
+    grouped(xcd_remap(id, tiles), tiles / tiles_v, tiles_v, &tn, &tv);
+    Place p;
+    p.tv = (int)tv;
+    p.tn = (int)tn;
+    p.c0 = (int)tv * Base::BM;
+    p.n0 = (int64_t)tn * Base::BN;
+    p.rows_v = min(Base::BM, classes - p.c0);
+    p.rows_n = min(Base::BN, count - (int)p.n0);
+    const Operand W{static_cast<const uint16_t*>(a.weight) + (int64_t)(first + p.c0) * a.D, a.D, p.rows_v};
+    const Operand X{a.packed + p.n0 * a.D, a.D, p.rows_n};
+    p.source = Base::source(W, X, a.D);
+    return p;
+  }
+  __device__ static inline uint32_t tiles(int count, int classes) {
+    return (uint32_t)((count + Base::BN - 1) / Base::BN) * (uint32_t)((classes + Base::BM - 1) / Base::BM);
+  }
 };
 
-template <int TM, int TN, int WGM, int WGN, int STAGES>
+template <int TM, int TN, int WGM, int WGN>
 __global__ __launch_bounds__(64 * WGM * WGN) void class_stats_kernel(ClassArgs a) {
-  using T = Logits<TM, TN, WGM, WGN, STAGES>;
+  using T = Logits<TM, TN, WGM, WGN>;
   __shared__ __attribute__((aligned(1024))) u32x4 lds[T::kLdsBytes / 16];
   const int count = uniform(*a.count);
-  const uint32_t tiles_v = (uint32_t)((a.V + T::BM - 1) / T::BM);
-  const uint32_t tile = xcd_remap(blockIdx.x, gridDim.x);
-  const uint32_t tn = tile / tiles_v, tv = tile - tn * tiles_v;
-  const int64_t n0 = (int64_t)tn * T::BN;
-  const int v0 = (int)tv * T::BM;
-  if (n0 >= count) return;
-  const int rows_n = (int)min((int64_t)T::BN, count - n0), rows_v = min(T::BM, a.V - v0);
+  const uint32_t tiles = T::tiles(count, a.V);
+  if (blockIdx.x >= tiles) return;
   const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
   const int wm = wave / WGN, wn = wave % WGN;
+  // beside the epilogue of a tile the next one's first slices are brought in; the epilogue has the ring's last place
+  float* part = reinterpret_cast<float*>(lds + 4 * T::kSlots);  // [WGM][BN][3]
+  static_assert(WGM * T::BN * 3 * 4 <= T::kPlaceBytes, "room in a place");
+  typename T::Place next = T::place(a, blockIdx.x, tiles, count, 0, a.V);
+  T::template fill<0, 4>(next.source, lds);
+  for (uint32_t id = blockIdx.x; id < tiles; id += gridDim.x) {
+  const typename T::Place at = next;
   f32x16 acc[TM][TN];
-  logits_tile<T>(a, v0, n0, rows_v, rows_n, lds, acc);
+  T::template run<4>(at.source, lds, acc);
+  const int v0 = at.c0, rows_v = at.rows_v, rows_n = at.rows_n;
+  const int64_t n0 = at.n0;
   const int first = v0 + wm * 32 * TM;
+  __syncthreads();  // every wavefront is done with the ring
+  if (id + gridDim.x < tiles) {
+    next = T::place(a, id + gridDim.x, tiles, count, 0, a.V);
+    T::template fill<0, 4>(next.source, lds);
+  }
   add_bias<TM, TN>(a.bias, first, a.V, lane, acc);
-
-  __syncthreads();  // every wavefront is done with the staged operands
-  float* part = reinterpret_cast<float*>(lds);  // [WGM][BN][3]
+  const int half = 4 * (lane >> 5);
+  const int classes = a.V - first - half;  // class 32 i + 8 (e / 4) + e % 4 of this lane exists if below
 #pragma unroll
   for (int j = 0; j < TN; ++j) {
     const int r = wn * 32 * TN + j * 32 + (lane & 31);
-    const int y = r < rows_n ? a.label_of[n0 + r] - first - 4 * (lane >> 5) : -1;
-    float m = kNegInf, sl = 0.f, own = 0.f;
-    bool has = false;
+    const int y = r < rows_n ? a.label_of[n0 + r] - first - half : -1;
+    float sl = 0.f;
+    if (a.logit_sums) {
+#pragma unroll
+      for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) sl += 32 * i + 8 * (e >> 2) + (e & 3) < classes ? acc[i][j][e] : 0.f;
+    }
+    if (rows_v < T::BM) {
+#pragma unroll
+      for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[i][j][e] = 32 * i + 8 * (e >> 2) + (e & 3) < classes ? acc[i][j][e] : kNegInf;
+    }
+    // the label's logit: few rows have theirs among a wavefront's classes
+    const bool mine = y >= 0 && y < 32 * TM && (y & 4) == 0;
+    if (__any(mine)) {
+      float own = 0.f;
+#pragma unroll
+      for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) own = 32 * i + 8 * (e >> 2) + (e & 3) == y ? acc[i][j][e] : own;
+      if (mine) a.label_logit[n0 + r] = own;
+    }
+    float m = acc[0][j][0];
 #pragma unroll
     for (int i = 0; i < TM; ++i)
 #pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const int c = 32 * i + 8 * (e >> 2) + (e & 3);
-        const float l = acc[i][j][e];
-        if (c == y) {
-          own = l;
-          has = true;
-        }
-        const bool in = first + 4 * (lane >> 5) + c < a.V;
-        m = in ? fmaxf(m, l) : m;
-        if (in) sl += l;
-      }
+      for (int e = 0; e < 16; ++e) m = fmaxf(m, acc[i][j][e]);
     m = fmaxf(m, __shfl_xor(m, 32, kWave));
+    const float from = m == kNegInf ? 0.f : m;  // (a tile of -inf only adds nothing; a NaN reaches the sum)
     float s = 0.f;
 #pragma unroll
     for (int i = 0; i < TM; ++i)
 #pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const int c = 32 * i + 8 * (e >> 2) + (e & 3);
-        const bool in = first + 4 * (lane >> 5) + c < a.V;
-        // (a NaN among the logits reaches the sum; a tile of -inf only adds nothing)
-        const float x = m == kNegInf && acc[i][j][e] == kNegInf ? 0.f : exp_neg(acc[i][j][e] - m);
-        if (in) s += x;
-      }
+      for (int e = 0; e < 16; ++e) s += exp_neg(acc[i][j][e] - from);
     s += __shfl_xor(s, 32, kWave);
     sl += __shfl_xor(sl, 32, kWave);
-    if (has) a.label_logit[n0 + r] = own;
     if (lane < 32) {
       float* p = part + (wm * T::BN + r) * 3;
       p[0] = m;
@@ -280,9 +314,11 @@ __global__ __launch_bounds__(64 * WGM * WGN) void class_stats_kernel(ClassArgs a
       s += p[0] == kNegInf ? p[1] : p[1] * exp_neg(p[0] - m);
       sl += p[2];
     }
-    float* out = a.stats + ((n0 + r) * (int64_t)tiles_v + tv) * 2;
-    *reinterpret_cast<f32x2*>(out) = f32x2{m, s};
-    if (a.logit_sums) a.logit_sums[(n0 + r) * (int64_t)tiles_v + tv] = sl;
+    const int64_t to = (n0 + r) * (int64_t)a.stat_tiles + at.tv;
+    reinterpret_cast<f32x2*>(a.stats)[to] = f32x2{m, s};
+    if (a.logit_sums) a.logit_sums[to] = sl;
+  }
+  __syncthreads();
   }
 }
 
@@ -350,59 +386,70 @@ __device__ inline void halve(float* v, int lane) {
   }
 }
 
-template <int TM, int TN, int WGM, int WGN, int STAGES>
+template <int TM, int TN, int WGM, int WGN>
 __global__ __launch_bounds__(64 * WGM * WGN) void class_grad_kernel(ClassArgs a) {
-  using T = Logits<TM, TN, WGM, WGN, STAGES>;
+  using T = Logits<TM, TN, WGM, WGN>;
   constexpr int kPitch = 32 * TM + 8;  // of a wavefront's strip of 32 rows, in fp16
   constexpr int kStripBytes = WGM * WGN * 32 * kPitch * 2;
-  constexpr int kColBytes = WGN * T::BM * 4;
-  constexpr int kBytes = T::kLdsBytes > kStripBytes + kColBytes ? T::kLdsBytes : kStripBytes + kColBytes;
-  __shared__ __attribute__((aligned(1024))) u32x4 lds[kBytes / 16];
+  static_assert(kStripBytes + WGN * T::BM * 4 <= 3 * T::kPlaceBytes, "room in three places");
+  __shared__ __attribute__((aligned(1024))) u32x4 lds[T::kLdsBytes / 16];
   const int count = uniform(*a.count);
-  const uint32_t tiles_v = (uint32_t)((a.piece_classes + T::BM - 1) / T::BM);
-  const uint32_t tile = xcd_remap(blockIdx.x, gridDim.x);
-  const uint32_t tn = tile / tiles_v, tv = tile - tn * tiles_v;
-  const int64_t n0 = (int64_t)tn * T::BN;
-  const int c0 = (int)tv * T::BM;  // of the piece
-  const int v0 = a.piece_first + c0;
-  if (n0 >= count) return;
-  const int rows_n = (int)min((int64_t)T::BN, count - n0), rows_v = min(T::BM, a.piece_classes - c0);
+  const uint32_t tiles = T::tiles(count, a.piece_classes);
+  if (blockIdx.x >= tiles) return;
   const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
   const int wm = wave / WGN, wn = wave % WGN;
+  // beside the epilogue of a tile the next one's first slice is brought in; the epilogue has the ring's last three places
+  char* room = reinterpret_cast<char*>(lds + 2 * T::kSlots);
+  uint16_t* strip = reinterpret_cast<uint16_t*>(room) + wave * 32 * kPitch;
+  float* columns = reinterpret_cast<float*>(room + kStripBytes);
+  typename T::Place next = T::place(a, blockIdx.x, tiles, count, a.piece_first, a.piece_classes);
+  T::template fill<0, 2>(next.source, lds);
+  for (uint32_t id = blockIdx.x; id < tiles; id += gridDim.x) {
+  const typename T::Place at = next;
   f32x16 acc[TM][TN];
-  logits_tile<T>(a, v0, n0, rows_v, rows_n, lds, acc);
-  const int first = v0 + wm * 32 * TM;
+  T::template run<2>(at.source, lds, acc);
+  const int c0 = at.c0, rows_v = at.rows_v, rows_n = at.rows_n;
+  const int64_t n0 = at.n0;
+  const int first = a.piece_first + c0 + wm * 32 * TM;
+  __syncthreads();  // every wavefront is done with the ring
+  if (id + gridDim.x < tiles) {
+    next = T::place(a, id + gridDim.x, tiles, count, a.piece_first, a.piece_classes);
+    T::template fill<0, 2>(next.source, lds);
+  }
   add_bias<TM, TN>(a.bias, first, a.V, lane, acc);
 
-  __syncthreads();
-  uint16_t* strip = reinterpret_cast<uint16_t*>(lds) + wave * 32 * kPitch;
-  float* columns = reinterpret_cast<float*>(reinterpret_cast<char*>(lds) + kStripBytes);
-  const float uniform = a.smoothing / (float)a.V;
-  const int end = a.piece_first + a.piece_classes;  // classes of the piece
+  const float uniform = a.smoothing / (float)a.V * kGScale, label = (1.0f - a.smoothing) * kGScale;
   const int half = 4 * (lane >> 5);
+  const int classes = a.piece_first + a.piece_classes - first - half;  // of the piece, from this lane's first one on
 #pragma unroll
   for (int j = 0; j < TN; ++j) {
     const int r = wn * 32 * TN + j * 32 + (lane & 31);
-    const bool live = r < rows_n;
-    const float m = live ? a.row_max[n0 + r] : 0.f, inv = live ? a.row_inv[n0 + r] : 0.f;
+    const bool live = r < rows_n;  // (a row that does not exist gets zeros)
+    const float m = live ? a.row_max[n0 + r] : __builtin_inff(), inv = live ? a.row_inv[n0 + r] * kGScale : 0.f;
+    const float off = live ? uniform : 0.f;
     const int y = live ? a.label_of[n0 + r] - first - half : -1;
 #pragma unroll
     for (int i = 0; i < TM; ++i)
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        float g[4];
+      for (int e = 0; e < 16; ++e) acc[i][j][e] = exp_neg(acc[i][j][e] - m) * inv - off;
+    if (__any(y >= 0 && y < 32 * TM)) {  // few rows have their label among a wavefront's classes
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const int c = 32 * i + 8 * q + k;
-          float v = exp_neg(acc[i][j][4 * q + k] - m) * inv - uniform;
-          if (c == y) v -= 1.0f - a.smoothing;
-          if (!live || first + half + c >= end) v = 0.f;
-          acc[i][j][4 * q + k] = v;
-          g[k] = v;
-        }
+      for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[i][j][e] -= 32 * i + 8 * (e >> 2) + (e & 3) == y ? label : 0.f;
+    }
+    if (rows_v < T::BM) {
+#pragma unroll
+      for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[i][j][e] = 32 * i + 8 * (e >> 2) + (e & 3) < classes ? acc[i][j][e] : 0.f;
+    }
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
         *reinterpret_cast<u32x2*>(strip + (lane & 31) * kPitch + 32 * i + 8 * q + half) =
-            u32x2{half_pair(g[0] * kGScale, g[1] * kGScale), half_pair(g[2] * kGScale, g[3] * kGScale)};
-      }
+            u32x2{half_pair(acc[i][j][4 * q], acc[i][j][4 * q + 1]), half_pair(acc[i][j][4 * q + 2], acc[i][j][4 * q + 3])};
     __builtin_amdgcn_wave_barrier();
     // rows of the strip to memory, 16 bytes per lane
     constexpr int kLanesPerRow = 4 * TM;
@@ -419,7 +466,7 @@ __global__ __launch_bounds__(64 * WGM * WGN) void class_grad_kernel(ClassArgs a)
     }
     __builtin_amdgcn_wave_barrier();
   }
-  if (!a.column_sums) return;
+  if (a.column_sums) {
   // sums over the tile's rows: over j in registers, over 32 lanes by halving, over wavefronts through LDS
   float v[16 * TM];
 #pragma unroll
@@ -460,7 +507,10 @@ __global__ __launch_bounds__(64 * WGM * WGN) void class_grad_kernel(ClassArgs a)
     float s = columns[c];
 #pragma unroll
     for (int w = 1; w < WGN; ++w) s += columns[w * T::BM + c];
-    a.column_sums[(int64_t)tn * a.piece_classes + c0 + c] = s;
+    a.column_sums[(int64_t)at.tn * a.piece_classes + c0 + c] = s;
+  }
+  }
+  __syncthreads();
   }
 }
 
@@ -544,7 +594,7 @@ __global__ __launch_bounds__(kFinishThreads) void class_bias_kernel(ClassArgs a)
   part[r][col] = s;
   __syncthreads();
   if (r == 0 && c < a.piece_classes)
-    a.grad_bias[a.piece_first + c] = ((part[0][col] + part[1][col]) + (part[2][col] + part[3][col])) * (float)grad_factor(a);
+    a.grad_bias[a.piece_first + c] = ((part[0][col] + part[1][col]) + (part[2][col] + part[3][col])) * (float)(grad_factor(a) / (double)kGScale);
 }
 
 }  // namespace
@@ -612,18 +662,22 @@ ClassPlan class_plan(int64_t M, int D, int V, bool grad) {
 }
 
 namespace {
-template <int TM, int TN, int WGM, int WGN, int STAGES>
-void launch_stats(const ClassArgs& a, hipStream_t stream) {
-  using T = Logits<TM, TN, WGM, WGN, STAGES>;
-  const int64_t tiles = ceil_div(a.M, T::BN) * ceil_div(a.V, T::BM);
-  hipLaunchKernelGGL((class_stats_kernel<TM, TN, WGM, WGN, STAGES>), dim3((uint32_t)tiles), dim3(T::kThreads), 0,
-                     stream, a);
+// Workgroups that walk the tiles: as many as fit on the compute units, or one per tile.
+template <class T>
+uint32_t walkers(int64_t M, int classes) {
+  const int64_t tiles = ceil_div(M, T::BN) * ceil_div(classes, T::BM);
+  constexpr int kPerUnit = 160 * 1024 / T::kLdsBytes;
+  return (uint32_t)(tiles < 256 * kPerUnit ? tiles : 256 * kPerUnit);
 }
-template <int TM, int TN, int WGM, int WGN, int STAGES>
+template <int TM, int TN, int WGM, int WGN>
+void launch_stats(const ClassArgs& a, hipStream_t stream) {
+  using T = Logits<TM, TN, WGM, WGN>;
+  hipLaunchKernelGGL((class_stats_kernel<TM, TN, WGM, WGN>), dim3(walkers<T>(a.M, a.V)), dim3(T::kThreads), 0, stream, a);
+}
+template <int TM, int TN, int WGM, int WGN>
 void launch_grad(const ClassArgs& a, hipStream_t stream) {
-  using T = Logits<TM, TN, WGM, WGN, STAGES>;
-  const int64_t tiles = ceil_div(a.M, T::BN) * ceil_div(a.piece_classes, T::BM);
-  hipLaunchKernelGGL((class_grad_kernel<TM, TN, WGM, WGN, STAGES>), dim3((uint32_t)tiles), dim3(T::kThreads), 0,
+  using T = Logits<TM, TN, WGM, WGN>;
+  hipLaunchKernelGGL((class_grad_kernel<TM, TN, WGM, WGN>), dim3(walkers<T>(a.M, a.piece_classes)), dim3(T::kThreads), 0,
                      stream, a);
 }
 uint32_t finish_blocks(int64_t values) {
@@ -639,9 +693,9 @@ hipError_t launch_class_loss(ClassArgs a, const ClassPlan& p, hipStream_t stream
   a.num_peaks = p.num_peaks;
   hipLaunchKernelGGL(class_pack_kernel, dim3((uint32_t)(a.peaks ? p.num_peaks : a.pack_blocks)), dim3(kPackThreads), 0,
                      stream, a);
-  if (p.side == 256) launch_stats<4, 2, 2, 4, 2>(a, stream);
-  else if (p.side == 128) launch_stats<2, 1, 2, 4, 2>(a, stream);
-  else launch_stats<1, 1, 2, 2, 3>(a, stream);
+  if (p.side == 256) launch_stats<4, 2, 2, 4>(a, stream);
+  else if (p.side == 128) launch_stats<2, 1, 2, 4>(a, stream);
+  else launch_stats<1, 1, 2, 2>(a, stream);
   hipLaunchKernelGGL(class_rows_kernel, dim3((uint32_t)p.num_partials), dim3(kRowThreads), 0, stream, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
@@ -659,9 +713,9 @@ hipError_t launch_class_loss(ClassArgs a, const ClassPlan& p, hipStream_t stream
   for (int first = 0; first < a.V; first += p.piece) {
     a.piece_first = first;
     a.piece_classes = a.V - first < p.piece ? a.V - first : p.piece;
-    if (p.side == 256) launch_grad<4, 2, 2, 4, 2>(a, stream);
-    else if (p.side == 128) launch_grad<2, 1, 2, 4, 2>(a, stream);
-    else launch_grad<1, 1, 2, 2, 3>(a, stream);
+    if (p.side == 256) launch_grad<4, 2, 2, 4>(a, stream);
+    else if (p.side == 128) launch_grad<2, 1, 2, 4>(a, stream);
+    else launch_grad<1, 1, 2, 2>(a, stream);
     e = hipGetLastError();
     if (e != hipSuccess) return e;
     const uint16_t* weight = a.half_weight + (int64_t)first * a.D;

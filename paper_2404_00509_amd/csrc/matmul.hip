@@ -12,9 +12,9 @@ namespace {
 
 using namespace mm;
 
-template <int TM, int TN, int WGM, int WGN, int STAGES, bool kAlongA, bool kHalf>
+template <int TM, int TN, int WGM, int WGN, bool kAlongA, bool kHalf>
 __global__ __launch_bounds__(64 * WGM * WGN) void matmul_kernel(MatmulArgs a) {
-  using T = Tile<TM, TN, WGM, WGN, STAGES, kAlongA, false, kHalf>;
+  using T = Tile<TM, TN, WGM, WGN, kAlongA, false, kHalf>;
   __shared__ __attribute__((aligned(1024))) u32x4 lds[T::kLdsBytes / 16];
   const int M = a.rows ? min(uniform(*a.rows), (int)a.M) : (int)a.M;
   const int K = a.depth ? min(uniform(*a.depth), (int)a.K) : (int)a.K;
@@ -34,7 +34,7 @@ __global__ __launch_bounds__(64 * WGM * WGN) void matmul_kernel(MatmulArgs a) {
   const Operand A{kAlongA ? a.A + m0 * a.lda + k0 : a.A + k0 * a.lda + m0, a.lda, rows_m};
   const Operand B{a.B + k0 * a.ldb + n0, a.ldb, rows_n};
   f32x16 acc[TM][TN];
-  T::run(A, B, depth, lds, acc);
+  T::template run<0>(T::source(A, B, depth), lds, acc);
 
   const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
   const int wm = wave / WGN, wn = wave % WGN;
@@ -57,13 +57,13 @@ __global__ __launch_bounds__(64 * WGM * WGN) void matmul_kernel(MatmulArgs a) {
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-template <int TM, int TN, int WGM, int WGN, int STAGES>
+template <int TM, int TN, int WGM, int WGN>
 void launch_sized(const MatmulArgs& a, bool along, bool half, hipStream_t stream) {
   constexpr int BM = 32 * TM * WGM, BN = 32 * TN * WGN;
   const dim3 grid((uint32_t)(ceil_div(a.M, BM) * ceil_div(a.N, BN) * a.parts)), block(64 * WGM * WGN);
-  if (along) hipLaunchKernelGGL((matmul_kernel<TM, TN, WGM, WGN, STAGES, true, true>), grid, block, 0, stream, a);
-  else if (half) hipLaunchKernelGGL((matmul_kernel<TM, TN, WGM, WGN, STAGES, false, true>), grid, block, 0, stream, a);
-  else hipLaunchKernelGGL((matmul_kernel<TM, TN, WGM, WGN, STAGES, false, false>), grid, block, 0, stream, a);
+  if (along) hipLaunchKernelGGL((matmul_kernel<TM, TN, WGM, WGN, true, true>), grid, block, 0, stream, a);
+  else if (half) hipLaunchKernelGGL((matmul_kernel<TM, TN, WGM, WGN, false, true>), grid, block, 0, stream, a);
+  else hipLaunchKernelGGL((matmul_kernel<TM, TN, WGM, WGN, false, false>), grid, block, 0, stream, a);
 }
 
 }  // namespace
@@ -84,9 +84,9 @@ int matmul_parts(int64_t M, int N, int64_t K, int side) {
 
 hipError_t launch_matmul(const MatmulArgs& a, MatmulKind kind, int side, hipStream_t stream) {
   const bool along = kind == MatmulKind::kHalfAlong, half = kind != MatmulKind::kBf16Across;
-  if (side == 256) launch_sized<4, 2, 2, 4, 2>(a, along, half, stream);
-  else if (side == 128) launch_sized<2, 1, 2, 4, 2>(a, along, half, stream);
-  else launch_sized<1, 1, 2, 2, 3>(a, along, half, stream);
+  if (side == 256) launch_sized<4, 2, 2, 4>(a, along, half, stream);
+  else if (side == 128) launch_sized<2, 1, 2, 4>(a, along, half, stream);
+  else launch_sized<1, 1, 2, 2>(a, along, half, stream);
   return hipGetLastError();
 }
 

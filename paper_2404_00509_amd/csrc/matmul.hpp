@@ -65,6 +65,30 @@ __device__ static inline const char* uniform(const uint16_t* p) {
   return reinterpret_cast<const char*>((uint64_t)(uint32_t)uniform((int)(v >> 32)) << 32 | (uint32_t)uniform((int)v));
 }
 
+// Tiles in the order in which workgroups take them: the rows of the grid of tiles in groups of kGroup, column by
+// column within a group, so that the 32 tiles that an XCD works on at a time share kGroup panels of one operand and
+// few of the other.
+constexpr uint32_t kGroup = 8;
+__device__ static inline void grouped(uint32_t id, uint32_t rows, uint32_t cols, uint32_t* row, uint32_t* col) {
+  const uint32_t group = id / (kGroup * cols);
+  const uint32_t first = group * kGroup, size = min(kGroup, rows - first);
+  const uint32_t in = id - first * cols;
+  *col = in / size;
+  *row = first + in - *col * size;
+}
+
+template <int v>
+struct Tag {
+  static constexpr int value = v;
+};
+template <int N, class F>
+__device__ static inline void unroll(F&& f) {
+  if constexpr (N > 0) {
+    unroll<N - 1>(f);
+    f(Tag<N - 1>{});
+  }
+}
+
 // One operand of a tile.
 struct Operand {
   const uint16_t* p;  // along k: element (first row of the tile, first k); across k: (first k, first column)
@@ -72,20 +96,27 @@ struct Operand {
   int limit;          // rows (along k) or columns (across k) of the tile that exist, at least 1
 };
 
-// A tile of (32 TM WGM) x (32 TN WGN) results by WGM x WGN wavefronts.
+// A tile of (32 TM WGM) x (32 TN WGN) results by WGM x WGN wavefronts, square.
 // Requirements: along k: k up to a multiple of 8 can be read and holds finite values where the other
 // operand's are zero; across k: whole chunks of 8 columns up to `limit` rounded up to 8 can be read
 // in every row.  Addresses are multiples of 4 bytes.
-template <int TM, int TN, int WGM, int WGN, int STAGES, bool kAlongA, bool kAlongB, bool kHalf = false>
+//
+// LDS is a ring of five places for a slice of one operand: A0 B0 A1 B1 A2, then B2 in A0's place, A3 in B0's and so
+// on.  When slice s is done, B of s + 2 is requested first, which has the whole of s + 1 to arrive, then A of
+// s + 3, which has two slices.  (With two places for both operands together, which is what fits with 256 x 256 results, the
+// last loads of a slice have a third of one.)
+template <int TM, int TN, int WGM, int WGN, bool kAlongA, bool kAlongB, bool kHalf = false>
 struct Tile {
   static constexpr int kThreads = 64 * WGM * WGN;
   static constexpr int BM = 32 * TM * WGM, BN = 32 * TN * WGN;
-  static constexpr int kSlotsA = BM * 8, kSlots = (BM + BN) * 8;  // 16-byte slots per stage
-  static constexpr int NL = kSlots / kThreads;                    // direct loads per lane and stage
-  static constexpr int kStageBytes = kSlots * 16;
-  static constexpr int kLdsBytes = STAGES * kStageBytes;
-  static_assert(kSlots % kThreads == 0 && kSlotsA % kWave == 0, "whole wave-wide loads of one operand");
-  static_assert(NL * (STAGES - 1) <= 63, "vmcnt range");
+  static_assert(BM == BN, "places of the ring hold either operand");
+  static constexpr int kSlots = BM * 8;         // 16-byte slots of a place
+  static constexpr int NL = kSlots / kThreads;  // direct loads per lane and place
+  static constexpr int kPlaceBytes = kSlots * 16;
+  static constexpr int kPlaces = 5;
+  static constexpr int kLdsBytes = kPlaces * kPlaceBytes;
+  static_assert(kSlots % kThreads == 0 && NL % 2 == 0, "halves of whole wave-wide loads");
+  static_assert(3 * NL <= 63, "vmcnt range");
 
   // which chunk of its row slot `s` of an operand of R rows or columns holds, and that row
   template <int R, bool kAlong>
@@ -100,83 +131,87 @@ struct Tile {
     }
   }
 
-  __device__ static inline void run(const Operand& A, const Operand& B, int K, u32x4* lds,
-                                    f32x16 (&acc)[TM][TN]) {
-    const int tid = threadIdx.x;
-    const int lane = tid % kWave;
-    const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+  // What a lane needs to bring in the slices of a tile's operands.
+  struct Source {
+    const char *a, *b;           // first slice
+    uint32_t step_a, step_b;     // bytes from slice to slice
+    uint32_t off_a[NL], off_b[NL];  // this lane's chunks of a slice
+    int K, nk, tail;
+  };
+  __device__ static inline Source source(const Operand& A, const Operand& B, int K) {
+    const int lane = threadIdx.x % kWave;
+    const int wave = uniform((int)threadIdx.x / kWave);
+    Source s;
+    s.a = uniform(A.p);
+    s.b = uniform(B.p);
+    s.step_a = kAlongA ? kSlice * 2 : kSlice * 2 * (uint32_t)uniform((int)A.ld);
+    s.step_b = kAlongB ? kSlice * 2 : kSlice * 2 * (uint32_t)uniform((int)B.ld);
+    s.K = K;
+    s.nk = (K + kSlice - 1) / kSlice;
+    s.tail = K % kSlice;
+#pragma unroll
+    for (int q = 0; q < NL; ++q) {
+      const int slot = (wave * NL + q) * kWave + lane;
+      int row, chunk;
+      slot_place<BM, kAlongA>(slot, &row, &chunk);
+      if (kAlongA) row = min(row, A.limit - 1);
+      else if (8 * chunk >= A.limit) chunk = 0;  // (any columns that exist: their results are not used)
+      s.off_a[q] = (uint32_t)(row * A.ld + 8 * chunk) * 2u;
+      slot_place<BN, kAlongB>(slot, &row, &chunk);
+      if (kAlongB) row = min(row, B.limit - 1);
+      else if (8 * chunk >= B.limit) chunk = 0;
+      s.off_b[q] = (uint32_t)(row * B.ld + 8 * chunk) * 2u;
+    }
+    return s;
+  }
+
+  // Loads q0 .. q1 of a slice of one operand into a place of the ring.
+  template <bool kA>
+  __device__ static inline void issue(const Source& s, u32x4* lds, int it, int place, int q0, int q1) {
+    constexpr bool kAlong = kA ? kAlongA : kAlongB;
+    const int lane = threadIdx.x % kWave;
+    const int wave = uniform((int)threadIdx.x / kWave);
+    u32x4* dst = lds + place * kSlots + wave * NL * kWave;
+    const char* base = (kA ? s.a : s.b) + (uint64_t)(uint32_t)it * (kA ? s.step_a : s.step_b);
+    asm("" : "+s"(base));
+#pragma unroll
+    for (int q = q0; q < q1; ++q) {
+      const char* src = base + (kA ? s.off_a[q] : s.off_b[q]);
+      if ((it + 1) * kSlice > s.K) {  // (a load for every lane, whatever it holds: the waits count them)
+        int row, chunk;
+        slot_place<BM, kAlong>((wave * NL + q) * kWave + lane, &row, &chunk);
+        if (kAlong ? 8 * chunk >= s.tail : row >= s.tail) src = reinterpret_cast<const char*>(&kZeros);
+      }
+      __builtin_amdgcn_global_load_lds((const void __attribute__((address_space(1)))*)src,
+                                       (void __attribute__((address_space(3)))*)(dst + q * kWave), 16, 0, 0);
+    }
+  }
+  // Slices `from` .. `to` of the ring's first five (A0 B0 A1 B1 A2), as far as there are any.
+  template <int kFrom, int kTo>
+  __device__ static inline void fill(const Source& s, u32x4* lds) {
+    unroll<kTo - kFrom>([&](auto tag) {
+      constexpr int n = kFrom + decltype(tag)::value;
+      if (n / 2 < s.nk) issue<n % 2 == 0>(s, lds, n / 2, n, 0, NL);
+    });
+  }
+
+  // The tile's sums.  kAhead: slices of the ring that fill() has been called for already (0, 2 or 4); no
+  // wavefront uses what the others' places hold any more.
+  template <int kAhead>
+  __device__ static inline void run(const Source& src, u32x4* lds, f32x16 (&acc)[TM][TN]) {
+    const int lane = threadIdx.x % kWave;
+    const int wave = uniform((int)threadIdx.x / kWave);
     const int wm = wave / WGN, wn = wave % WGN;
+    const int nk = src.nk, tail = src.tail;
 #pragma unroll
     for (int i = 0; i < TM; ++i)
 #pragma unroll
       for (int j = 0; j < TN; ++j)
 #pragma unroll
         for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
-    const int nk = (K + kSlice - 1) / kSlice;
     if (nk == 0) return;
-    const int tail = K % kSlice;
 
-    // what this lane brings in per stage, as bytes from the operand's first element of the slice
-    uint32_t off[NL];
-#pragma unroll
-    for (int q = 0; q < NL; ++q) {
-      const int s0 = (wave * NL + q) * kWave;  // (the same operand for all lanes)
-      int row, chunk;
-      if (s0 < kSlotsA) {
-        slot_place<BM, kAlongA>(s0 + lane, &row, &chunk);
-        if (kAlongA) row = min(row, A.limit - 1);
-        else if (8 * chunk >= A.limit) chunk = 0;  // (any columns that exist: their results are not used)
-        off[q] = (uint32_t)(row * A.ld + 8 * chunk) * 2u;
-      } else {
-        slot_place<BN, kAlongB>(s0 - kSlotsA + lane, &row, &chunk);
-        if (kAlongB) row = min(row, B.limit - 1);
-        else if (8 * chunk >= B.limit) chunk = 0;
-        off[q] = (uint32_t)(row * B.ld + 8 * chunk) * 2u;
-      }
-    }
-    // bytes from slice to slice
-    const uint32_t step_a = kAlongA ? kSlice * 2 : kSlice * 2 * (uint32_t)uniform((int)A.ld);
-    const uint32_t step_b = kAlongB ? kSlice * 2 : kSlice * 2 * (uint32_t)uniform((int)B.ld);
-    const char* const first_a = uniform(A.p);
-    const char* const first_b = uniform(B.p);
-
-    auto issue = [&](int it, int stage, int q0, int q1) {
-      u32x4* dst = lds + stage * kSlots + wave * NL * kWave;
-      const char* a_base = first_a + (uint64_t)(uint32_t)it * step_a;
-      const char* b_base = first_b + (uint64_t)(uint32_t)it * step_b;
-      asm("" : "+s"(a_base), "+s"(b_base));
-      if ((it + 1) * kSlice <= K) {
-#pragma unroll
-        for (int q = q0; q < q1; ++q) {
-          const char* base = (wave * NL + q) * kWave < kSlotsA ? a_base : b_base;
-          __builtin_amdgcn_global_load_lds((const void __attribute__((address_space(1)))*)(base + off[q]),
-                                           (void __attribute__((address_space(3)))*)(dst + q * kWave), 16, 0, 0);
-        }
-      } else {
-        // (a load for every lane, whatever it holds: the waits count them)
-#pragma unroll
-        for (int q = q0; q < q1; ++q) {
-          const int s0 = (wave * NL + q) * kWave;
-          int row, chunk;
-          bool behind;
-          const char* src;
-          if (s0 < kSlotsA) {
-            slot_place<BM, kAlongA>(s0 + lane, &row, &chunk);
-            behind = kAlongA ? 8 * chunk >= tail : row >= tail;
-            src = a_base + off[q];
-          } else {
-            slot_place<BN, kAlongB>(s0 - kSlotsA + lane, &row, &chunk);
-            behind = kAlongB ? 8 * chunk >= tail : row >= tail;
-            src = b_base + off[q];
-          }
-          if (behind) src = reinterpret_cast<const char*>(&kZeros);
-          __builtin_amdgcn_global_load_lds((const void __attribute__((address_space(1)))*)src,
-                                           (void __attribute__((address_space(3)))*)(dst + q * kWave), 16, 0, 0);
-        }
-      }
-    };
-
-    // fragment addresses inside a stage (bytes)
+    // fragment addresses inside a place (bytes)
     const uint32_t lds_base = (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) u32x4*)lds;
     const uint32_t c0 = (uint32_t)((lane >> 5) ^ ((lane >> 1) & 7)) * 16u;
     const int g = lane >> 4, i16 = lane & 15;
@@ -188,18 +223,24 @@ struct Tile {
       for (int t = 0; t < TM; ++t) fa_at[t] = lds_base + across_at<BM>(wm * TM + t, g, i16);
     }
     if constexpr (kAlongB) {
-      fb_at[0] = lds_base + (uint32_t)(BM + wn * 32 * TN + (lane & 31)) * 128u + c0;
+      fb_at[0] = lds_base + (uint32_t)(wn * 32 * TN + (lane & 31)) * 128u + c0;
     } else {
 #pragma unroll
-      for (int t = 0; t < TN; ++t) fb_at[t] = lds_base + BM * 128 + across_at<BN>(wn * TN + t, g, i16);
+      for (int t = 0; t < TN; ++t) fb_at[t] = lds_base + across_at<BN>(wn * TN + t, g, i16);
     }
 
     u32x4 fa[2][TM], fb[2][TN];
-    auto read_frags = [&](int stage, auto ks_tag, int set) {
-      constexpr int ks = decltype(ks_tag)::value;
-      const uint32_t st = (uint32_t)stage * kStageBytes;
-      read_operand<BM, TM, kAlongA, ks>(fa_at, st, fa[set]);
-      read_operand<BN, TN, kAlongB, ks>(fb_at, st, fb[set]);
+    // Read number r of sub-step ks: the operands' reads one after the other.
+    constexpr int kReadsA = kAlongA ? TM : 2 * TM, kReadsB = kAlongB ? TN : 2 * TN, kReads = kReadsA + kReadsB;
+    auto read_one = [&](uint32_t a_bytes, uint32_t b_bytes, auto ks_tag, auto r_tag, int set) {
+      constexpr int ks = decltype(ks_tag)::value, r = decltype(r_tag)::value;
+      if constexpr (r < kReadsA) read_part<BM, kAlongA, ks, r>(fa_at, a_bytes, fa[set]);
+      else read_part<BN, kAlongB, ks, r - kReadsA>(fb_at, b_bytes, fb[set]);
+    };
+    auto read_frags = [&](int a_place, int b_place, auto ks_tag, int set) {
+      unroll<kReads>([&](auto r) {
+        read_one((uint32_t)a_place * kPlaceBytes, (uint32_t)b_place * kPlaceBytes, ks_tag, r, set);
+      });
       __builtin_amdgcn_sched_barrier(0);
     };
     auto arrive = [&](int set) {
@@ -210,92 +251,101 @@ struct Tile {
 #pragma unroll
       for (int j = 0; j < TN; ++j) asm volatile("" : "+v"(fb[set][j]));
     };
-    auto multiply = [&](int set, int from, int to) {
-#pragma unroll
-      for (int i = from; i < to; ++i)
-#pragma unroll
-        for (int j = 0; j < TN; ++j)
-          if constexpr (kHalf)
-            acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, fa[set][i]),
-                                                               __builtin_bit_cast(f16x8, fb[set][j]), acc[i][j], 0, 0,
-                                                               0);
-          else
-            acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, fa[set][i]),
-                                                                __builtin_bit_cast(bf16x8, fb[set][j]), acc[i][j], 0,
-                                                                0, 0);
+    auto multiply_one = [&](int set, int i, int j) {
+      if constexpr (kHalf)
+        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, fa[set][i]),
+                                                           __builtin_bit_cast(f16x8, fb[set][j]), acc[i][j], 0, 0, 0);
+      else
+        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, fa[set][i]),
+                                                            __builtin_bit_cast(bf16x8, fb[set][j]), acc[i][j], 0, 0, 0);
     };
-    // slice `next` has landed for all wavefronts, and all have read what they need of the one before
-    auto turn = [&](int next) {
-      if (next + STAGES - 1 <= nk) __builtin_amdgcn_s_waitcnt(wait_vm(NL * (STAGES - 2)));
-      else __builtin_amdgcn_s_waitcnt(wait_vm(0));
-      __builtin_amdgcn_s_barrier();
+    auto multiply = [&](int set) {
+#pragma unroll
+      for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j) multiply_one(set, i, j);
+    };
+    // The multiplies of one set of fragments; behind each of the first ones a share of the reads of the other set
+    // (sub-step ks of the slice in these places), behind the last ones `loads`, one by one.
+    constexpr int kMul = TM * TN;
+    constexpr int kReadMul = kMul >= 8 ? kMul * 3 / 4 : kMul;  // multiplies that reads follow
+    auto step = [&](int set, int a_place, int b_place, auto ks_tag, auto&& load) {
+      const uint32_t a_bytes = (uint32_t)a_place * kPlaceBytes, b_bytes = (uint32_t)b_place * kPlaceBytes;
+      unroll<kMul>([&](auto m_tag) {
+        constexpr int m = decltype(m_tag)::value;
+        multiply_one(set, m / TN, m % TN);
+        __builtin_amdgcn_sched_barrier(0);
+        constexpr int r0 = m < kReadMul ? kReads * m / kReadMul : kReads;
+        constexpr int r1 = m < kReadMul ? kReads * (m + 1) / kReadMul : kReads;
+        unroll<r1 - r0>([&](auto r) {
+          read_one(a_bytes, b_bytes, ks_tag, Tag<r0 + decltype(r)::value>{}, set ^ 1);
+        });
+        constexpr int l0 = (NL / 2) * m / kMul, l1 = (NL / 2) * (m + 1) / kMul;
+        if constexpr (l1 > l0) load(l0, l1);
+        __builtin_amdgcn_sched_barrier(0);
+      });
+      arrive(set ^ 1);
     };
 
-#pragma unroll
-    for (int s = 0; s < STAGES; ++s)
-      if (s < nk) issue(s, s, 0, NL);
-    if (nk >= STAGES) __builtin_amdgcn_s_waitcnt(wait_vm(NL * (STAGES - 1)));
+    fill<kAhead, 5>(src, lds);
+    // slice 0 has landed; of what was issued here the rest may be on its way
+    static_assert(kAhead == 0 || kAhead == 2 || kAhead == 4, "whole slices of both operands");
+    constexpr int kRest = kAhead == 4 ? 1 : 3;
+    if (nk > 2) __builtin_amdgcn_s_waitcnt(wait_vm(kRest * NL));
+    else if (nk > 1) __builtin_amdgcn_s_waitcnt(wait_vm((kRest - 1) * NL));
     else __builtin_amdgcn_s_waitcnt(wait_vm(0));
     __builtin_amdgcn_s_barrier();
-    read_frags(0, Tag<0>{}, 0);
+    read_frags(0, 1, Tag<0>{}, 0);
     arrive(0);
 
     // A slice is four sub-steps of 16 k; the fragments of a sub-step are read while the one before it is
-    // multiplied, across slices too; the loads that refill a stage come in three parts.
-    constexpr int kLoads1 = 3 * NL / 8, kLoads2 = 6 * NL / 8;
-    int cur = 0;
+    // multiplied, across slices too; the loads that refill the ring are spread over all four.
+    int pa = 0;  // place of A of this slice; B's is the next one
     for (int it = 0; it + 1 < nk; ++it) {
-      const bool more = it >= 1 && it + STAGES - 1 < nk;
-      const int prv = cur == 0 ? STAGES - 1 : cur - 1;
-      auto sub = [&](auto ks_tag) {
-        constexpr int ks = decltype(ks_tag)::value;
-        read_frags(cur, Tag<ks + 1>{}, (ks + 1) & 1);
-        multiply(ks & 1, 0, 1);
-        __builtin_amdgcn_sched_barrier(0);
-        if (more && ks == 0) issue(it + STAGES - 1, prv, kLoads1, kLoads2);
-        if (more && ks == 1) issue(it + STAGES - 1, prv, kLoads2, NL);
-        __builtin_amdgcn_sched_barrier(0);
-        multiply(ks & 1, 1, TM);
-        arrive((ks + 1) & 1);
-      };
-      sub(Tag<0>{});
-      sub(Tag<1>{});
-      sub(Tag<2>{});
-      const int nxt = cur + 1 == STAGES ? 0 : cur + 1;
-      turn(it + 1);
-      read_frags(nxt, Tag<0>{}, 0);
-      multiply(1, 0, 1);
-      __builtin_amdgcn_sched_barrier(0);
-      if (it + STAGES < nk) issue(it + STAGES, cur, 0, kLoads1);
-      __builtin_amdgcn_sched_barrier(0);
-      multiply(1, 1, TM);
-      arrive(0);
-      cur = nxt;
+      const int pb = pa + 1 == kPlaces ? 0 : pa + 1;
+      const int na = pb + 1 == kPlaces ? 0 : pb + 1, nb = na + 1 == kPlaces ? 0 : na + 1;  // of the next slice
+      const int ma = nb + 1 == kPlaces ? 0 : nb + 1;                                       // A of the one after it
+      constexpr int kHalfNL = NL / 2;
+      step(0, pa, pb, Tag<1>{}, [&](int q0, int q1) {
+        if (it >= 1) issue<false>(src, lds, it + 1, nb, kHalfNL + q0, kHalfNL + q1);
+      });
+      step(1, pa, pb, Tag<2>{}, [&](int q0, int q1) {
+        if (it >= 1 && it + 2 < nk) issue<true>(src, lds, it + 2, ma, q0, q1);
+      });
+      step(0, pa, pb, Tag<3>{}, [&](int q0, int q1) {
+        if (it >= 1 && it + 2 < nk) issue<true>(src, lds, it + 2, ma, kHalfNL + q0, kHalfNL + q1);
+      });
+      // the next slice has landed (the A behind it may be on its way) for all wavefronts, and all have read what
+      // they need of this one
+      if (it + 2 < nk) __builtin_amdgcn_s_waitcnt(wait_vm(NL));
+      else __builtin_amdgcn_s_waitcnt(wait_vm(0));
+      __builtin_amdgcn_s_barrier();
+      step(1, na, nb, Tag<0>{}, [&](int q0, int q1) {  // (B of slice it + 2 goes where A of this one was)
+        if (it + 2 < nk) issue<false>(src, lds, it + 2, pa, q0, q1);
+      });
+      pa = na;
     }
+    const int pb = pa + 1 == kPlaces ? 0 : pa + 1;
     const int left = tail ? (tail + 15) / 16 : 4;  // sub-steps of the last slice that hold values
-    if (left > 1) read_frags(cur, Tag<1>{}, 1);
-    multiply(0, 0, TM);
+    if (left > 1) read_frags(pa, pb, Tag<1>{}, 1);
+    multiply(0);
     if (left > 1) {
       arrive(1);
-      if (left > 2) read_frags(cur, Tag<2>{}, 0);
-      multiply(1, 0, TM);
+      if (left > 2) read_frags(pa, pb, Tag<2>{}, 0);
+      multiply(1);
     }
     if (left > 2) {
       arrive(0);
-      if (left > 3) read_frags(cur, Tag<3>{}, 1);
-      multiply(0, 0, TM);
+      if (left > 3) read_frags(pa, pb, Tag<3>{}, 1);
+      multiply(0);
     }
     if (left > 3) {
       arrive(1);
-      multiply(1, 0, TM);
+      multiply(1);
     }
   }
 
  private:
-  template <int v>
-  struct Tag {
-    static constexpr int value = v;
-  };
   // where lane (g, i) of a 32-column block reads: row i / 4 of its group of four, columns 16 (g % 2) + 4 (i % 4)
   template <int R>
   __device__ static inline uint32_t across_at(int block, int g, int i) {
@@ -304,21 +354,15 @@ struct Tile {
     const int chunk = (block * 4 + (g & 1) * 2 + ((i & 3) >> 1)) ^ swizzle;
     return (uint32_t)(k * R * 2 + chunk * 16 + (i & 1) * 8);
   }
-  template <int R, int T, bool kAlong, int ks, int N>
-  __device__ static inline void read_operand(const uint32_t (&at)[N], uint32_t st, u32x4 (&f)[T]) {
+  template <int R, bool kAlong, int ks, int r, int T, int N>
+  __device__ static inline void read_part(const uint32_t (&at)[N], uint32_t place, u32x4 (&f)[T]) {
     if constexpr (kAlong) {
-      const uint32_t v = (at[0] ^ (32u * ks)) + st;
-      f[0] = read_along<0>(v);
-      if constexpr (T >= 2) f[1] = read_along<4096>(v);
-      if constexpr (T >= 3) f[2] = read_along<8192>(v);
-      if constexpr (T >= 4) f[3] = read_along<12288>(v);
+      f[r] = read_along<r * 4096>((at[0] ^ (32u * ks)) + place);
     } else {
-#pragma unroll
-      for (int t = 0; t < T; ++t) {
-        const u32x2 lo = read_across<ks * 32 * R>(at[t] + st);
-        const u32x2 hi = read_across<ks * 32 * R + 8 * R>(at[t] + st);
-        f[t] = u32x4{lo.x, lo.y, hi.x, hi.y};
-      }
+      constexpr int t = r / 2;
+      const u32x2 v = read_across<ks * 32 * R + (r % 2) * 8 * R>(at[t] + place);
+      if constexpr (r % 2 == 0) f[t] = u32x4{v.x, v.y, f[t].z, f[t].w};
+      else f[t] = u32x4{f[t].x, f[t].y, v.x, v.y};
     }
   }
 };
