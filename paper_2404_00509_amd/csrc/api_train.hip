@@ -195,18 +195,23 @@ int mae_class_loss(const mae_class_desc* d, float* loss, float* row_loss, void* 
   a.grad_tokens = grad_tokens;
   a.grad_weight = grad_weight;
   a.grad_bias = grad_bias;
-  a.count = at(p.count, (int32_t*)nullptr);
-  a.slot_of = at(p.slot_of, (int32_t*)nullptr);
-  a.label_of = at(p.label_of, (int32_t*)nullptr);
-  a.packed = at(p.packed, (uint16_t*)nullptr);
   a.stats = at(p.stats, (float*)nullptr);
   a.logit_sums = d->smoothing > 0.0f ? at(p.logit_sums, (float*)nullptr) : nullptr;
   a.label_logit = at(p.label_logit, (float*)nullptr);
-  a.row_max = at(p.row_max, (float*)nullptr);
-  a.row_inv = at(p.row_inv, (float*)nullptr);
-  a.partials = at(p.partials, (double*)nullptr);
+  if (p.few) {  // the tokens and labels as they are
+    a.packed = const_cast<uint16_t*>(static_cast<const uint16_t*>(d->tokens));
+    a.label_of = const_cast<int32_t*>(d->labels);
+  } else {
+    a.count = at(p.count, (int32_t*)nullptr);
+    a.label_of = at(p.label_of, (int32_t*)nullptr);
+    a.row_of = at(p.row_of, (int32_t*)nullptr);
+    a.packed = at(p.packed, (uint16_t*)nullptr);
+    a.partials = at(p.partials, (double*)nullptr);
+  }
   if (grad) {
     a.peaks = at(p.peaks, (int32_t*)nullptr);
+    a.row_max = at(p.row_max, (float*)nullptr);
+    a.row_inv = at(p.row_inv, (float*)nullptr);
     a.half_tokens = at(p.half_tokens, (uint16_t*)nullptr);
     a.half_weight = at(p.half_weight, (uint16_t*)nullptr);
     a.g = at(p.g, (uint16_t*)nullptr);

@@ -7,16 +7,19 @@
 //   g = (softmax(l) - (1 - s) onehot(y) - s / V) grad_scale / count
 //   grad_x = g W, grad_W = g^T x, grad_b = sum over rows of g
 //
-//   pack    rows whose label is no class are left out: the others' numbers, labels and tokens one after the
-//           other, and their count, which the later kernels read from memory.  What such a row holds (NaN, infinities)
-//           touches nothing.  For the gradient also the largest magnitudes among tokens and weight
-//   stats   tiles of logits -> per row and tile the maximum, the sum of exponentials under it, the sum of logits
-//           (smoothing) and the label's logit
-//   rows    the tiles of a row joined -> maximum, 1 / sum, the row's loss
-//   halves  tokens and weight as fp16
-//   grad    tiles of logits again -> g as fp16 [rows, classes of the piece], sums of its columns in fp32
-//   matmul  g W (g along k, W across k) and g^T x (both across k); few tiles: k is split
-//   finish  the parts of a split joined, scaled, rounded once to bf16
+//   pack      rows whose label is no class are left out: the others' labels and tokens one after the other, and
+//             their count, which the later kernels read from memory.  What such a row holds (NaN, infinities) touches
+//             nothing.  For the gradient also the largest magnitudes among tokens and weight
+//   stats     tiles of logits -> per row and tile the maximum, the sum of exponentials under it, the sum of logits
+//             (smoothing) and the label's logit
+//   rows      the tiles of a row joined -> maximum, 1 / sum, the row's loss.  Beside it, for the gradient, tokens and
+//             weight as fp16
+//   grad      tiles of logits again -> g as fp16 [rows, classes of the piece], sums of its columns in fp32; one
+//             workgroup joins the loss (without gradient: a launch of its own)
+//   products  g W (g along k, W across k) and g^T x (both across k) in one launch; few tiles: k is split
+//   finish    grad_bias, and the parts of a split joined, scaled, rounded once to bf16
+//
+// The loss alone of a few rows (one tile of 64) takes two launches: stats on the tokens as they are, rows.
 //
 // The gradient goes through the vocabulary in pieces, so g takes M x piece values of the workspace.
 // Logits are made as W x^T: a lane then holds up to 64 classes of one row, and the
@@ -39,14 +42,19 @@ namespace {
 using namespace mm;
 
 typedef f32x4 f32x4_a4 __attribute__((aligned(4)));
+typedef int32_t i32x4_a4 __attribute__((ext_vector_type(4), aligned(4)));
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kNegInf = -__builtin_inff();
+constexpr float kGScale = 32768.0f;  // of g as fp16
 
 // exp(v) for v <= 0
 __device__ inline float exp_neg(float v) { return __builtin_amdgcn_exp2f(v * kLog2e); }
 
-// ---- pack -----------------------------------------------------------------------------------------
+// rows that take part
+__device__ inline int row_count(const ClassArgs& a) { return a.count ? uniform(*a.count) : (int)a.M; }
+
+// ---- powers of two that bring the operands into the range of fp16 ---------------------------------------
 constexpr int kPackThreads = 256;
 
 // The larger of `peak` and the finite magnitudes among eight bf16 values, as bits.
@@ -86,6 +94,30 @@ __device__ inline int32_t peak_among(const int32_t* peaks, int from, int to) {
   return p;
 }
 
+__device__ inline uint32_t half_pair(float lo, float hi) {
+  typedef float in2 __attribute__((ext_vector_type(2)));
+  typedef _Float16 out2 __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector((in2{lo, hi}), out2));
+}
+
+// grad_scale / count
+__device__ inline double grad_factor(const ClassArgs& a) {
+  const int n = *a.count;
+  return n > 0 ? (double)a.grad_scale / (double)n : 0.0;
+}
+// A product's sum to a gradient, with the powers of two of its operands taken out: `rest` is the factor of the
+// operand beside g.  (That factor may be as far from 1 as floats go, so it is not multiplied into `factor`.)
+struct Scale {
+  float factor;
+  int rest;
+  __device__ inline float operator()(float v) const { return ldexpf(v * factor, rest); }
+};
+__device__ inline Scale product_scale(const ClassArgs& a, bool by_weight) {
+  const int from = by_weight ? a.pack_blocks : 0, to = by_weight ? a.num_peaks : a.pack_blocks;
+  return Scale{(float)(grad_factor(a) / (double)kGScale), -half_exponent(peak_among(a.peaks, from, to))};
+}
+
+// ---- pack -----------------------------------------------------------------------------------------
 // Workgroups from pack_blocks on look for the largest magnitude of the weight.
 __global__ __launch_bounds__(kPackThreads) void class_pack_kernel(ClassArgs a) {
   __shared__ int32_t wave_sum[kPackThreads / kWave];
@@ -94,19 +126,28 @@ __global__ __launch_bounds__(kPackThreads) void class_pack_kernel(ClassArgs a) {
   int32_t peak = 0;
   if ((int)blockIdx.x >= a.pack_blocks) {
     const u32x4* w = reinterpret_cast<const u32x4*>(a.weight);
-    const int64_t n = (int64_t)a.V * a.D / 8;
-    for (int64_t i = (int64_t)((int)blockIdx.x - a.pack_blocks) * kPackThreads + tid; i < n;
-         i += (int64_t)(a.num_peaks - a.pack_blocks) * kPackThreads)
-      peak = peak_of(peak, w[i]);
+    const int64_t n = (int64_t)a.V * a.D / 8, step = (int64_t)(a.num_peaks - a.pack_blocks) * kPackThreads;
+    constexpr int kBatch = 4;  // loads in flight
+    for (int64_t i = (int64_t)((int)blockIdx.x - a.pack_blocks) * kPackThreads + tid; i < n; i += kBatch * step) {
+      u32x4 v[kBatch];
+#pragma unroll
+      for (int k = 0; k < kBatch; ++k) v[k] = i + k * step < n ? w[i + k * step] : u32x4{0u, 0u, 0u, 0u};
+#pragma unroll
+      for (int k = 0; k < kBatch; ++k) peak = peak_of(peak, v[k]);
+    }
     leave_peak(peak, wave_sum, a.peaks + blockIdx.x);
     return;
   }
   const int64_t row0 = (int64_t)blockIdx.x * a.pack_rows;
   const int64_t end = min(row0 + a.pack_rows, a.M);
-  auto is_class = [&](int64_t r) { return (uint32_t)a.labels[r] < (uint32_t)a.V; };
-  // rows in front of this workgroup's that take part
+  auto is_class = [&](int32_t label) { return (uint32_t)label < (uint32_t)a.V ? 1 : 0; };
+  // rows in front of this workgroup's that take part (row0 is a multiple of 4)
   int32_t before = 0;
-  for (int64_t r = tid; r < row0; r += kPackThreads) before += is_class(r) ? 1 : 0;
+#pragma unroll 4
+  for (int64_t r = 4 * tid; r < row0; r += 4 * kPackThreads) {
+    const i32x4_a4 l = *reinterpret_cast<const i32x4_a4*>(a.labels + r);
+    before += (is_class(l.x) + is_class(l.y)) + (is_class(l.z) + is_class(l.w));
+  }
 #pragma unroll
   for (int off = kWave / 2; off > 0; off >>= 1) before += __shfl_xor(before, off, kWave);
   if (lane == 0) wave_sum[wave] = before;
@@ -115,7 +156,7 @@ __global__ __launch_bounds__(kPackThreads) void class_pack_kernel(ClassArgs a) {
   for (int w = 0; w < kPackThreads / kWave; ++w) at += wave_sum[w];
   for (int64_t base = row0; base < end; base += kPackThreads) {
     const int64_t r = base + tid;
-    const bool in = r < end && is_class(r);
+    const bool in = r < end && is_class(a.labels[r]);
     const uint64_t votes = __ballot(in);
     __syncthreads();
     if (lane == 0) wave_sum[wave] = __popcll(votes);
@@ -123,49 +164,33 @@ __global__ __launch_bounds__(kPackThreads) void class_pack_kernel(ClassArgs a) {
     int32_t slot = at + __popcll(votes & ((1ull << lane) - 1));
     for (int w = 0; w < wave; ++w) slot += wave_sum[w];
     for (int w = 0; w < kPackThreads / kWave; ++w) at += wave_sum[w];
-    if (r < end) a.slot_of[r] = in ? slot : -1;
-    if (in) a.label_of[slot] = a.labels[r];
+    if (in) {
+      a.label_of[slot] = a.labels[r];
+      a.row_of[slot] = (int32_t)r;
+    }
+    if (r < end && !in && a.row_loss) a.row_loss[r] = 0.f;
     map[tid] = in ? slot : -1;
     __syncthreads();
     // the tokens, a wavefront per row, 16 bytes per lane
     const int rows = (int)min((int64_t)kPackThreads, end - base);
     for (int i = wave; i < rows; i += kPackThreads / kWave) {
       const int32_t to = map[i];
-      if (to < 0) continue;
-      const u32x4* src = reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(a.tokens) + (base + i) * a.D);
-      u32x4* dst = reinterpret_cast<u32x4*>(a.packed + (int64_t)to * a.D);
-      for (int c = lane; c < a.D / 8; c += kWave) {
-        const u32x4 v = src[c];
-        if (a.peaks) peak = peak_of(peak, v);
-        dst[c] = v;
+      if (to >= 0) {
+        const u32x4* src = reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(a.tokens) + (base + i) * a.D);
+        u32x4* dst = reinterpret_cast<u32x4*>(a.packed + (int64_t)to * a.D);
+        for (int c = lane; c < a.D / 8; c += kWave) {
+          const u32x4 v = src[c];
+          if (a.peaks) peak = peak_of(peak, v);
+          dst[c] = v;
+        }
+      } else if (a.grad_tokens) {
+        u32x4* dst = reinterpret_cast<u32x4*>(static_cast<uint16_t*>(a.grad_tokens) + (base + i) * a.D);
+        for (int c = lane; c < a.D / 8; c += kWave) dst[c] = u32x4{0u, 0u, 0u, 0u};
       }
     }
   }
   if (end == a.M && tid == 0) *a.count = at;
   if (a.peaks) leave_peak(peak, wave_sum, a.peaks + blockIdx.x);
-}
-
-// ---- halves: eight values per lane -----------------------------------------------------------------
-__device__ inline uint32_t half_pair(float lo, float hi) {
-  typedef float in2 __attribute__((ext_vector_type(2)));
-  typedef _Float16 out2 __attribute__((ext_vector_type(2)));
-  return __builtin_bit_cast(uint32_t, __builtin_convertvector((in2{lo, hi}), out2));
-}
-__global__ __launch_bounds__(kPackThreads) void class_halves_kernel(ClassArgs a) {
-  const int64_t of_tokens = (int64_t)*a.count * (a.D / 8), of_weight = (int64_t)a.V * (a.D / 8);
-  const float ft = ldexpf(1.0f, half_exponent(peak_among(a.peaks, 0, a.pack_blocks)));
-  const float fw = ldexpf(1.0f, half_exponent(peak_among(a.peaks, a.pack_blocks, a.num_peaks)));
-  for (int64_t i = (int64_t)blockIdx.x * kPackThreads + threadIdx.x; i < of_tokens + of_weight;
-       i += (int64_t)gridDim.x * kPackThreads) {
-    const bool t = i < of_tokens;
-    const int64_t at = t ? i : i - of_tokens;
-    const u32x4 v = t ? reinterpret_cast<const u32x4*>(a.packed)[at] : reinterpret_cast<const u32x4*>(a.weight)[at];
-    const float f = t ? ft : fw;
-    u32x4 out;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) out[k] = half_pair(bf16_lo(v[k]) * f, bf16_hi(v[k]) * f);
-    reinterpret_cast<u32x4*>(t ? a.half_tokens : a.half_weight)[at] = out;
-  }
 }
 
 // ---- tiles of logits --------------------------------------------------------------------------------
@@ -230,7 +255,7 @@ template <int TM, int TN, int WGM, int WGN>
 __global__ __launch_bounds__(64 * WGM * WGN) void class_stats_kernel(ClassArgs a) {
   using T = Logits<TM, TN, WGM, WGN>;
   __shared__ __attribute__((aligned(1024))) u32x4 lds[T::kLdsBytes / 16];
-  const int count = uniform(*a.count);
+  const int count = row_count(a);
   const uint32_t tiles = T::tiles(count, a.V);
   if (blockIdx.x >= tiles) return;
   const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
@@ -322,53 +347,111 @@ __global__ __launch_bounds__(64 * WGM * WGN) void class_stats_kernel(ClassArgs a
   }
 }
 
-// ---- rows: a wavefront each --------------------------------------------------------------------------
-constexpr int kRowThreads = 256;
+// ---- rows -------------------------------------------------------------------------------------------
+// One row by one wavefront: its loss; maximum and 1 / sum to memory.
+__device__ inline float join_row(const ClassArgs& a, int64_t slot, int lane) {
+  const f32x2* st = reinterpret_cast<const f32x2*>(a.stats) + slot * a.stat_tiles;
+  float m = kNegInf, s = 0.f, sl = 0.f;
+  for (int t = lane; t < a.stat_tiles; t += kWave) m = fmaxf(m, st[t].x);
+#pragma unroll
+  for (int off = kWave / 2; off > 0; off >>= 1) m = fmaxf(m, __shfl_xor(m, off, kWave));
+  for (int t = lane; t < a.stat_tiles; t += kWave) {
+    const f32x2 p = st[t];
+    s += p.x == kNegInf ? p.y : p.y * exp_neg(p.x - m);
+    if (a.logit_sums) sl += a.logit_sums[slot * a.stat_tiles + t];
+  }
+#pragma unroll
+  for (int off = kWave / 2; off > 0; off >>= 1) {
+    s += __shfl_xor(s, off, kWave);
+    sl += __shfl_xor(sl, off, kWave);
+  }
+  float v = (m + logf(s)) - (1.0f - a.smoothing) * a.label_logit[slot];
+  if (a.logit_sums) v -= a.smoothing * (sl / (float)a.V);
+  if (lane == 0 && a.peaks) {
+    a.row_max[slot] = m;
+    a.row_inv[slot] = 1.0f / s;
+  }
+  return v;
+}
+
+constexpr int kRowThreads = 256, kRowWaves = kRowThreads / kWave;
+// Workgroups from row_blocks on make the fp16 copies, eight values per lane.
 __global__ __launch_bounds__(kRowThreads) void class_rows_kernel(ClassArgs a) {
-  __shared__ double sums[kRowThreads / kWave];
-  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-  const int64_t row = (int64_t)blockIdx.x * (kRowThreads / kWave) + wave;
-  double loss = 0.0;
-  if (row < a.M) {
-    const int slot = a.slot_of[row];
-    if (slot >= 0) {
-      const f32x2* st = reinterpret_cast<const f32x2*>(a.stats) + (int64_t)slot * a.stat_tiles;
-      float m = kNegInf, s = 0.f, sl = 0.f;
-      for (int t = lane; t < a.stat_tiles; t += kWave) m = fmaxf(m, st[t].x);
+  if ((int)blockIdx.x >= a.row_blocks) {
+    const int64_t of_tokens = (int64_t)*a.count * (a.D / 8), of_weight = (int64_t)a.V * (a.D / 8);
+    const float ft = ldexpf(1.0f, half_exponent(peak_among(a.peaks, 0, a.pack_blocks)));
+    const float fw = ldexpf(1.0f, half_exponent(peak_among(a.peaks, a.pack_blocks, a.num_peaks)));
+    const int64_t step = (int64_t)((int)gridDim.x - a.row_blocks) * kRowThreads;
+    for (int64_t i = (int64_t)((int)blockIdx.x - a.row_blocks) * kRowThreads + threadIdx.x; i < of_tokens + of_weight;
+         i += step) {
+      const bool t = i < of_tokens;
+      const int64_t at = t ? i : i - of_tokens;
+      const u32x4 v = t ? reinterpret_cast<const u32x4*>(a.packed)[at] : reinterpret_cast<const u32x4*>(a.weight)[at];
+      const float f = t ? ft : fw;
+      u32x4 out;
 #pragma unroll
-      for (int off = kWave / 2; off > 0; off >>= 1) m = fmaxf(m, __shfl_xor(m, off, kWave));
-      for (int t = lane; t < a.stat_tiles; t += kWave) {
-        const f32x2 p = st[t];
-        s += p.x == kNegInf ? p.y : p.y * exp_neg(p.x - m);
-        if (a.logit_sums) sl += a.logit_sums[(int64_t)slot * a.stat_tiles + t];
-      }
-#pragma unroll
-      for (int off = kWave / 2; off > 0; off >>= 1) {
-        s += __shfl_xor(s, off, kWave);
-        sl += __shfl_xor(sl, off, kWave);
-      }
-      float v = (m + logf(s)) - (1.0f - a.smoothing) * a.label_logit[slot];
-      if (a.logit_sums) v -= a.smoothing * (sl / (float)a.V);
-      loss = (double)v;
-      if (lane == 0) {
-        a.row_max[slot] = m;
-        a.row_inv[slot] = 1.0f / s;
-      }
+      for (int k = 0; k < 4; ++k) out[k] = half_pair(bf16_lo(v[k]) * f, bf16_hi(v[k]) * f);
+      reinterpret_cast<u32x4*>(t ? a.half_tokens : a.half_weight)[at] = out;
     }
-    if (lane == 0 && a.row_loss) a.row_loss[row] = (float)loss;
+    return;
+  }
+  __shared__ double sums[kRowWaves];
+  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+  const int count = *a.count;
+  double loss = 0.0;
+  for (int64_t slot = (int64_t)blockIdx.x * kRowWaves + wave; slot < count; slot += (int64_t)a.row_blocks * kRowWaves) {
+    const float v = join_row(a, slot, lane);
+    loss += (double)v;
+    if (lane == 0 && a.row_loss) a.row_loss[a.row_of[slot]] = v;
   }
   if (lane == 0) sums[wave] = loss;
   __syncthreads();
-  if (threadIdx.x == 0) {
-    double s = 0.0;
-    for (int w = 0; w < kRowThreads / kWave; ++w) s += sums[w];
-    a.partials[blockIdx.x] = s;
+  if (threadIdx.x == 0) a.partials[blockIdx.x] = (sums[0] + sums[1]) + (sums[2] + sums[3]);
+}
+
+// The loss from the workgroups' shares, by the first kRowThreads threads of a workgroup; `sums`: kRowWaves of LDS.
+__device__ inline void join_losses(const ClassArgs& a, double* sums) {
+  const int tid = threadIdx.x, count = *a.count;
+  double s = 0.0;
+  if (tid < kRowThreads)
+    for (int i = tid; i < a.row_blocks; i += kRowThreads) s += a.partials[i];
+#pragma unroll
+  for (int off = kWave / 2; off > 0; off >>= 1) s += __shfl_xor(s, off, kWave);
+  if (tid < kRowThreads && tid % kWave == 0) sums[tid / kWave] = s;
+  __syncthreads();
+  if (tid == 0) *a.loss = count > 0 ? (float)(((sums[0] + sums[1]) + (sums[2] + sums[3])) / (double)count) : 0.f;
+  __syncthreads();
+}
+__global__ __launch_bounds__(kRowThreads) void class_loss_kernel(ClassArgs a) {
+  __shared__ double sums[kRowWaves];
+  join_losses(a, sums);
+}
+
+// The rows of a call that did not pack any: one workgroup.
+constexpr int kFewThreads = 1024, kFewRows = 64;
+__global__ __launch_bounds__(kFewThreads) void class_few_rows_kernel(ClassArgs a) {
+  __shared__ double losses[kFewRows];
+  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+  int n = 0;
+  for (int64_t row = wave; row < a.M; row += kFewThreads / kWave) {
+    const bool in = (uint32_t)a.labels[row] < (uint32_t)a.V;
+    const float v = in ? join_row(a, row, lane) : 0.f;
+    if (lane == 0) {
+      losses[row] = (double)v;
+      if (a.row_loss) a.row_loss[row] = v;
+    }
   }
+  __syncthreads();
+  if (threadIdx.x > 0) return;
+  double s = 0.0;
+  for (int64_t row = 0; row < a.M; ++row) {
+    s += losses[row];
+    n += (uint32_t)a.labels[row] < (uint32_t)a.V ? 1 : 0;
+  }
+  *a.loss = n > 0 ? (float)(s / (double)n) : 0.f;
 }
 
 // ---- the gradient of the logits, one piece of the classes -------------------------------------------------
-constexpr float kGScale = 32768.0f;  // of g as fp16
-
 // One step of adding kCount values over the 32 lanes of half a wavefront: lanes whose bit kMask is set go on
 // with the upper half of the values, the others with the lower half.
 template <int kCount, int kMask>
@@ -395,6 +478,8 @@ __global__ __launch_bounds__(64 * WGM * WGN) void class_grad_kernel(ClassArgs a)
   __shared__ __attribute__((aligned(1024))) u32x4 lds[T::kLdsBytes / 16];
   const int count = uniform(*a.count);
   const uint32_t tiles = T::tiles(count, a.piece_classes);
+  // (with the first piece: the loss, by a workgroup that has no more tiles than any other)
+  if (a.piece_first == 0 && blockIdx.x == gridDim.x - 1) join_losses(a, reinterpret_cast<double*>(lds));
   if (blockIdx.x >= tiles) return;
   const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
   const int wm = wave / WGN, wn = wave % WGN;
@@ -514,87 +599,161 @@ __global__ __launch_bounds__(64 * WGM * WGN) void class_grad_kernel(ClassArgs a)
   }
 }
 
-// ---- finish -----------------------------------------------------------------------------------------
-__device__ inline double grad_factor(const ClassArgs& a) {
-  const int n = *a.count;
-  return n > 0 ? (double)a.grad_scale / (double)n : 0.0;
-}
-// A product's sum to a gradient, with the powers of two of its operands taken out: `rest` is the factor of the
-// operand beside g.  (That factor may be as far from 1 as floats go, so it is not multiplied into `factor`.)
-struct Scale {
-  float factor;
-  int rest;
-  __device__ inline float operator()(float v) const { return ldexpf(v * factor, rest); }
+// ---- products ---------------------------------------------------------------------------------------
+// Part s of the sums over k of A(m, k) B[k][n], B with k as its row number; k is split into parts.
+struct Product {
+  const uint16_t* A;  // "along": A[m][k]; otherwise A[k][m]
+  const uint16_t* B;
+  int64_t lda, ldb;   // values from row to row
+  int M, N, K, parts;
+  const int32_t* rows;    // nullable: only so many m (device memory)
+  const int32_t* depth;   // nullable: only so many k
+  float* acc;             // [parts][M][N]
+  bool accumulate;        // to what is there
+  uint16_t* out;          // nullable: with one part, bf16 results instead of sums
+  const int32_t* row_of;  // nullable: rows of `out` that the m go to
+  bool by_weight;         // B is the weight's copy (tokens' otherwise)
 };
-__device__ inline Scale product_scale(const ClassArgs& a, int from, int to) {
-  return Scale{(float)(grad_factor(a) / (double)kGScale), -half_exponent(peak_among(a.peaks, from, to))};
-}
-__device__ inline u32x4 pack8(const float (&v)[8]) {
-  return u32x4{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])};
-}
-// eight values at `at` of the first of `parts` arrays that lie `stride` values apart, added up
-__device__ inline void sum_parts(const float* p, int64_t at, int64_t stride, int parts, float (&v)[8]) {
+
+template <int TM, int TN, int WGM, int WGN, bool kAlongA>
+__device__ inline void product_tile(const ClassArgs& a, const Product& p, uint32_t block, uint32_t blocks, u32x4* lds) {
+  using T = Tile<TM, TN, WGM, WGN, kAlongA, false, true>;
+  const int M = p.rows ? min(uniform(*p.rows), p.M) : p.M;
+  const int K = p.depth ? min(uniform(*p.depth), p.K) : p.K;
+  const uint32_t tiles_n = (uint32_t)((p.N + T::BN - 1) / T::BN);
+  const uint32_t tiles = (uint32_t)((p.M + T::BM - 1) / T::BM) * tiles_n;
+  const uint32_t id = xcd_remap(block, blocks);
+  const uint32_t part = id / tiles, tile = id - part * tiles;
+  const uint32_t tm = tile / tiles_n, tn = tile - tm * tiles_n;
+  const int m0 = (int)tm * T::BM, n0 = (int)tn * T::BN;
+  if (m0 >= M) return;
+  const int rows_m = min(T::BM, M - m0), rows_n = min(T::BN, p.N - n0);
+  // this part's share of the slices of k
+  const int slices = (K + kSlice - 1) / kSlice, share = (slices + p.parts - 1) / p.parts;
+  const int s0 = uniform(min((int)part * share, slices)), s1 = uniform(min(s0 + share, slices));
+  const int64_t k0 = (int64_t)s0 * kSlice;
+  const int depth = uniform(min(s1 * kSlice, K) - min(s0 * kSlice, K));
+  const Operand A{kAlongA ? p.A + m0 * p.lda + k0 : p.A + k0 * p.lda + m0, p.lda, rows_m};
+  const Operand B{p.B + k0 * p.ldb + n0, p.ldb, rows_n};
+  f32x16 acc[TM][TN];
+  T::template run<0>(T::source(A, B, depth), lds, acc);
+
+  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+  const int wm = wave / WGN, wn = wave % WGN;
+  float* sums = p.acc + ((int64_t)part * p.M + m0) * p.N + n0;
+  const bool final = p.out && p.parts == 1;
+  if (!final || p.accumulate) {
 #pragma unroll
-  for (int k = 0; k < 8; ++k) v[k] = 0.f;
-  for (int s = 0; s < parts; ++s) {
-    const f32x4 lo = *reinterpret_cast<const f32x4*>(p + s * stride + at);
-    const f32x4 hi = *reinterpret_cast<const f32x4*>(p + s * stride + at + 4);
+    for (int i = 0; i < TM; ++i)
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      v[k] += lo[k];
-      v[4 + k] += hi[k];
+      for (int e = 0; e < 16; ++e) {
+        const int r = wm * 32 * TM + 32 * i + 8 * (e >> 2) + 4 * (lane >> 5) + (e & 3);
+        if (r >= rows_m) continue;
+#pragma unroll
+        for (int j = 0; j < TN; ++j) {
+          const int c = wn * 32 * TN + 32 * j + (lane & 31);
+          if (c >= rows_n) continue;
+          float* at = sums + (int64_t)r * p.N + c;
+          if (p.accumulate) acc[i][j][e] += *at;
+          if (!final) *at = acc[i][j][e];
+        }
+      }
+    if (!final) return;
+  }
+  // results through a strip of LDS per wavefront, 32 rows at a time: 16 bytes per lane along a row (N is a multiple of 8)
+  const Scale scaled = product_scale(a, p.by_weight);
+  constexpr int kPitch = 32 * TN + 8;
+  static_assert(WGM * WGN * 32 * kPitch * 2 <= T::kLdsBytes, "room for the strips");
+  uint16_t* strip = reinterpret_cast<uint16_t*>(lds) + wave * 32 * kPitch;
+  __syncthreads();  // every wavefront is done with the staged operands
+#pragma unroll
+  for (int i = 0; i < TM; ++i) {
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int j = 0; j < TN; ++j)
+#pragma unroll
+      for (int e = 0; e < 16; ++e)
+        strip[(8 * (e >> 2) + 4 * (lane >> 5) + (e & 3)) * kPitch + 32 * j + (lane & 31)] =
+            (uint16_t)bf16_rne(scaled(acc[i][j][e]));
+    __builtin_amdgcn_wave_barrier();
+    constexpr int kLanesPerRow = 4 * TN, kRowsPerRep = kWave / kLanesPerRow;
+#pragma unroll
+    for (int rep = 0; rep < 32 / kRowsPerRep; ++rep) {
+      const int sr = rep * kRowsPerRep + lane / kLanesPerRow, col = (lane % kLanesPerRow) * 8;
+      const int r = wm * 32 * TM + 32 * i + sr, c = wn * 32 * TN + col;
+      if (r >= rows_m || c >= rows_n) continue;
+      const int64_t row = p.row_of ? p.row_of[m0 + r] : m0 + r;
+      *reinterpret_cast<u32x4*>(p.out + row * p.N + n0 + c) = *reinterpret_cast<const u32x4*>(strip + sr * kPitch + col);
     }
   }
 }
 
+// The first `of_tokens` workgroups make g W, the others g^T x.
+template <int TM, int TN, int WGM, int WGN>
+__global__ __launch_bounds__(64 * WGM * WGN) void class_products_kernel(ClassArgs a, Product tokens, Product weight,
+                                                                        uint32_t of_tokens) {
+  __shared__ __attribute__((aligned(1024))) u32x4 lds[Tile<TM, TN, WGM, WGN, true, false, true>::kLdsBytes / 16];
+  if (blockIdx.x < of_tokens) product_tile<TM, TN, WGM, WGN, true>(a, tokens, blockIdx.x, of_tokens, lds);
+  else product_tile<TM, TN, WGM, WGN, false>(a, weight, blockIdx.x - of_tokens, gridDim.x - of_tokens, lds);
+}
+
+// ---- finish -----------------------------------------------------------------------------------------
 constexpr int kFinishThreads = 256;
-// grad_tokens: eight values per lane
-__global__ __launch_bounds__(kFinishThreads) void class_tokens_kernel(ClassArgs a) {
+
+// eight values at `at` of the first of `parts` arrays that lie `stride` values apart, added up and scaled, as bf16
+__device__ inline u32x4 joined(const float* p, int64_t at, int64_t stride, int parts, const Scale& scaled) {
+  f32x4 lo = f32x4{0.f, 0.f, 0.f, 0.f}, hi = lo;
+  for (int s = 0; s < parts; ++s) {
+    lo += *reinterpret_cast<const f32x4*>(p + s * stride + at);
+    hi += *reinterpret_cast<const f32x4*>(p + s * stride + at + 4);
+  }
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    lo[k] = scaled(lo[k]);
+    hi[k] = scaled(hi[k]);
+  }
+  return u32x4{pack_bf16x2(lo.x, lo.y), pack_bf16x2(lo.z, lo.w), pack_bf16x2(hi.x, hi.y), pack_bf16x2(hi.z, hi.w)};
+}
+
+// Workgroups [0, for_bias): grad_bias of the piece, 64 classes by four wavefronts.  [for_bias, + for_weight):
+// grad_weight of the piece from its parts.  The rest: grad_tokens from its parts.
+__global__ __launch_bounds__(kFinishThreads) void class_finish_kernel(ClassArgs a, uint32_t for_bias, uint32_t for_weight) {
   const int per_row = a.D / 8;
-  const Scale scaled = product_scale(a, a.pack_blocks, a.num_peaks);
-  const int64_t total = a.M * per_row;
-  for (int64_t i = (int64_t)blockIdx.x * kFinishThreads + threadIdx.x; i < total;
-       i += (int64_t)gridDim.x * kFinishThreads) {
-    const int64_t row = i / per_row;
-    const int c = (int)(i - row * per_row) * 8;
-    const int slot = a.slot_of[row];
-    float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    if (slot >= 0) {
-      sum_parts(a.tokens_acc, (int64_t)slot * a.D + c, a.M * a.D, a.tokens_parts, v);
-#pragma unroll
-      for (int k = 0; k < 8; ++k) v[k] = scaled(v[k]);
-    }
-    *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(a.grad_tokens) + row * a.D + c) = pack8(v);
+  uint32_t block = blockIdx.x;
+  if (block < for_bias) {
+    __shared__ float part[4][64];
+    const int col = threadIdx.x % 64, r = threadIdx.x / 64;
+    const int c = (int)block * 64 + col;
+    const int tiles = (*a.count + a.grad_rows - 1) / a.grad_rows;
+    float s = 0.f;
+    if (c < a.piece_classes)
+      for (int t = r; t < tiles; t += 4) s += a.column_sums[(int64_t)t * a.piece_classes + c];
+    part[r][col] = s;
+    __syncthreads();
+    if (r == 0 && c < a.piece_classes)
+      a.grad_bias[a.piece_first + c] = ((part[0][col] + part[1][col]) + (part[2][col] + part[3][col])) *
+                                       (float)(grad_factor(a) / (double)kGScale);
+    return;
   }
-}
-
-// grad_weight of the piece
-__global__ __launch_bounds__(kFinishThreads) void class_weight_kernel(ClassArgs a) {
-  const Scale scaled = product_scale(a, 0, a.pack_blocks);
-  const int64_t stride = (int64_t)a.piece_classes * a.D, total = stride / 8;
-  for (int64_t i = (int64_t)blockIdx.x * kFinishThreads + threadIdx.x; i < total;
-       i += (int64_t)gridDim.x * kFinishThreads) {
-    float v[8];
-    sum_parts(a.weight_acc, i * 8, stride, a.weight_parts, v);
-#pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] = scaled(v[k]);
-    *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(a.grad_weight) + (int64_t)a.piece_first * a.D + i * 8) = pack8(v);
+  block -= for_bias;
+  if (block < for_weight) {
+    const Scale scaled = product_scale(a, false);
+    const int64_t total = (int64_t)a.piece_classes * per_row;
+    for (int64_t i = (int64_t)block * kFinishThreads + threadIdx.x; i < total; i += (int64_t)for_weight * kFinishThreads)
+      *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(a.grad_weight) + (int64_t)a.piece_first * a.D + i * 8) =
+          joined(a.weight_acc, i * 8, (int64_t)a.piece_classes * a.D, a.weight_parts, scaled);
+    return;
   }
-}
-
-// grad_bias of the piece: 64 classes by 4 lanes each
-__global__ __launch_bounds__(kFinishThreads) void class_bias_kernel(ClassArgs a) {
-  __shared__ float part[4][64];
-  const int col = threadIdx.x % 64, r = threadIdx.x / 64;
-  const int c = blockIdx.x * 64 + col;
-  const int tiles = (*a.count + a.grad_rows - 1) / a.grad_rows;
-  float s = 0.f;
-  if (c < a.piece_classes)
-    for (int t = r; t < tiles; t += 4) s += a.column_sums[(int64_t)t * a.piece_classes + c];
-  part[r][col] = s;
-  __syncthreads();
-  if (r == 0 && c < a.piece_classes)
-    a.grad_bias[a.piece_first + c] = ((part[0][col] + part[1][col]) + (part[2][col] + part[3][col])) * (float)(grad_factor(a) / (double)kGScale);
+  block -= for_weight;
+  const uint32_t blocks = gridDim.x - for_bias - for_weight;
+  const Scale scaled = product_scale(a, true);
+  const int64_t total = (int64_t)*a.count * per_row;
+  for (int64_t i = (int64_t)block * kFinishThreads + threadIdx.x; i < total; i += (int64_t)blocks * kFinishThreads) {
+    const int64_t slot = i / per_row;
+    const int c = (int)(i - slot * per_row) * 8;
+    *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(a.grad_tokens) + (int64_t)a.row_of[slot] * a.D + c) =
+        joined(a.tokens_acc, slot * a.D + c, a.M * a.D, a.tokens_parts, scaled);
+  }
 }
 
 }  // namespace
@@ -612,22 +771,30 @@ int logits_side(int64_t M, int V) {
   return 256;
 }
 
+// Parts that k is split into: as many as give every compute unit a tile, of four slices at least.
+int product_parts(int64_t M, int N, int64_t K, int side, int64_t slots) {
+  const int64_t tiles = ceil_div(M, side) * ceil_div(N, side);
+  int64_t parts = slots / tiles;
+  if (parts > ceil_div(K, kSlice) / 4) parts = ceil_div(K, kSlice) / 4;
+  return parts < 1 ? 1 : (int)parts;
+}
+
 }  // namespace
+
+// Side of the tiles of the two products of a piece.
+static int products_side(int64_t M, int D, int V) {
+  if (M <= 64 || V <= 64) return 64;
+  const int64_t tiles = ceil_div(M, 256) * ceil_div(D, 256) + ceil_div(V, 256) * ceil_div(D, 256);
+  return tiles < 256 ? 128 : 256;
+}
 
 ClassPlan class_plan(int64_t M, int D, int V, bool grad) {
   ClassPlan p{};
+  p.few = !grad && M <= kFewRows;
   p.side = logits_side(M, V);
   p.stat_tiles = (int)ceil_div(V, p.side);
-  p.pack_rows = (int)ceil_div(ceil_div(M, 1024), 64) * 64;
-  // g of a piece takes at most 512 MiB, or 1024 classes
-  const int64_t most = (int64_t(1) << 28) / M / 256 * 256;
-  p.piece = (int)(most < 1024 ? 1024 : most < V ? most : V);
-  if (p.piece > V) p.piece = V;
-  p.piece_ld = (int)ceil_div(p.piece, 64) * 64;
-  p.tokens_side = matmul_side(M, D);
-  p.tokens_parts = matmul_parts(M, D, p.piece, p.tokens_side);
-  p.weight_side = matmul_side(p.piece, D);
-  p.weight_parts = matmul_parts(p.piece, D, M, p.weight_side);
+  p.pack_rows = (int)ceil_div(ceil_div(M, 1024), 16) * 16;
+  p.row_blocks = (int)(ceil_div(M, kRowWaves) < 2048 ? ceil_div(M, kRowWaves) : 2048);
   size_t at = 0;
   const auto take = [&](size_t bytes) {
     const size_t was = at;
@@ -635,27 +802,38 @@ ClassPlan class_plan(int64_t M, int D, int V, bool grad) {
     return was;
   };
   const size_t m = (size_t)M;
-  p.count = take(sizeof(int32_t));
-  p.slot_of = take(m * 4);
-  p.label_of = take(m * 4);
-  p.packed = take(m * D * 2);
   p.stats = take(m * p.stat_tiles * 8);
   p.logit_sums = take(m * p.stat_tiles * 4);
   p.label_logit = take(m * 4);
-  p.row_max = take(m * 4);
-  p.row_inv = take(m * 4);
-  p.num_partials = (int)ceil_div(M, kRowThreads / kWave);
-  p.partials = take((size_t)p.num_partials * 8);
+  if (!p.few) {
+    p.count = take(sizeof(int32_t));
+    p.label_of = take(m * 4);
+    p.row_of = take(m * 4);
+    p.packed = take(m * D * 2);
+    p.partials = take((size_t)p.row_blocks * 8);
+  }
   if (grad) {
-    p.num_weight_peaks = (int)min(ceil_div((int64_t)V * D / 8, kPackThreads * 4), (int64_t)512);
+    // g of a piece takes at most 512 MiB, or 1024 classes
+    const int64_t most = (int64_t(1) << 28) / M / 256 * 256;
+    p.piece = (int)(most < 1024 ? 1024 : most < V ? most : V);
+    if (p.piece > V) p.piece = V;
+    p.piece_ld = (int)ceil_div(p.piece, 64) * 64;
+    p.products_side = products_side(M, D, p.piece);
+    const int64_t slots = p.products_side == 256 ? 256 : p.products_side == 128 ? 256 : 512;
+    p.tokens_parts = product_parts(M, D, p.piece, p.products_side, slots);
+    p.weight_parts = product_parts(p.piece, D, M, p.products_side, slots);
+    p.num_weight_peaks = (int)(ceil_div((int64_t)V * D / 8, kPackThreads * 4) < 1024
+                                   ? ceil_div((int64_t)V * D / 8, kPackThreads * 4) : 1024);
     p.num_peaks = (int)ceil_div(M, p.pack_rows) + p.num_weight_peaks;
     p.peaks = take((size_t)p.num_peaks * 4);
+    p.row_max = take(m * 4);
+    p.row_inv = take(m * 4);
     p.half_tokens = take(m * D * 2);
     p.half_weight = take((size_t)V * D * 2);
     p.g = take(m * p.piece_ld * 2);
     p.column_sums = take((size_t)ceil_div(M, p.side) * p.piece * 4);
-    p.tokens_acc = take(m * D * 4 * p.tokens_parts);
-    p.weight_acc = take((size_t)p.piece * D * 4 * p.weight_parts);
+    if (p.tokens_parts > 1 || p.piece < V) p.tokens_acc = take(m * D * 4 * p.tokens_parts);
+    if (p.weight_parts > 1) p.weight_acc = take((size_t)p.piece * D * 4 * p.weight_parts);
   }
   p.bytes = at;
   return p;
@@ -680,9 +858,19 @@ void launch_grad(const ClassArgs& a, hipStream_t stream) {
   hipLaunchKernelGGL((class_grad_kernel<TM, TN, WGM, WGN>), dim3(walkers<T>(a.M, a.piece_classes)), dim3(T::kThreads), 0,
                      stream, a);
 }
+template <int TM, int TN, int WGM, int WGN>
+void launch_products(const ClassArgs& a, const Product& tokens, const Product& weight, hipStream_t stream) {
+  constexpr int BM = 32 * TM * WGM, BN = 32 * TN * WGN;
+  const auto blocks = [&](const Product& p) {
+    return p.A ? (uint32_t)(ceil_div(p.M, BM) * ceil_div(p.N, BN) * p.parts) : 0u;
+  };
+  const uint32_t of_tokens = blocks(tokens), of_weight = blocks(weight);
+  hipLaunchKernelGGL((class_products_kernel<TM, TN, WGM, WGN>), dim3(of_tokens + of_weight), dim3(64 * WGM * WGN), 0,
+                     stream, a, tokens, weight, of_tokens);
+}
 uint32_t finish_blocks(int64_t values) {
   const int64_t blocks = ceil_div(values / 8, kFinishThreads);
-  return (uint32_t)(blocks < 1 ? 1 : blocks < 65536 ? blocks : 65536);
+  return (uint32_t)(blocks < 1 ? 1 : blocks < 2048 ? blocks : 2048);
 }
 }  // namespace
 
@@ -691,20 +879,26 @@ hipError_t launch_class_loss(ClassArgs a, const ClassPlan& p, hipStream_t stream
   a.stat_tiles = p.stat_tiles;
   a.pack_blocks = (int)ceil_div(a.M, p.pack_rows);
   a.num_peaks = p.num_peaks;
-  hipLaunchKernelGGL(class_pack_kernel, dim3((uint32_t)(a.peaks ? p.num_peaks : a.pack_blocks)), dim3(kPackThreads), 0,
-                     stream, a);
+  a.row_blocks = p.row_blocks;
+  const bool grad = a.peaks != nullptr;
+  if (!p.few)
+    hipLaunchKernelGGL(class_pack_kernel, dim3((uint32_t)(grad ? p.num_peaks : a.pack_blocks)), dim3(kPackThreads), 0,
+                       stream, a);
   if (p.side == 256) launch_stats<4, 2, 2, 4>(a, stream);
   else if (p.side == 128) launch_stats<2, 1, 2, 4>(a, stream);
   else launch_stats<1, 1, 2, 2>(a, stream);
-  hipLaunchKernelGGL(class_rows_kernel, dim3((uint32_t)p.num_partials), dim3(kRowThreads), 0, stream, a);
+  if (p.few) {
+    hipLaunchKernelGGL(class_few_rows_kernel, dim3(1), dim3(kFewThreads), 0, stream, a);
+    return hipGetLastError();
+  }
+  const int64_t for_halves = ceil_div((a.M + a.V) * a.D / 8, kRowThreads);
+  hipLaunchKernelGGL(class_rows_kernel,
+                     dim3((uint32_t)(p.row_blocks + (grad ? (for_halves < 4096 ? for_halves : 4096) : 0))),
+                     dim3(kRowThreads), 0, stream, a);
+  if (!grad) hipLaunchKernelGGL(class_loss_kernel, dim3(1), dim3(kRowThreads), 0, stream, a);
   hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  e = launch_loss_finish(a.partials, p.num_partials, 0.0, a.loss, a.count, 1, 1, stream);
-  if (e != hipSuccess) return e;
-  if (!a.grad_tokens && !a.grad_weight && !a.grad_bias) return hipSuccess;
+  if (e != hipSuccess || !grad) return e;
 
-  hipLaunchKernelGGL(class_halves_kernel, dim3((uint32_t)min(ceil_div((a.M + a.V) * a.D / 8, kPackThreads), (int64_t)4096)),
-                     dim3(kPackThreads), 0, stream, a);
   a.piece_ld = p.piece_ld;
   a.grad_rows = p.side;
   a.tokens_parts = p.tokens_parts;
@@ -713,40 +907,41 @@ hipError_t launch_class_loss(ClassArgs a, const ClassPlan& p, hipStream_t stream
   for (int first = 0; first < a.V; first += p.piece) {
     a.piece_first = first;
     a.piece_classes = a.V - first < p.piece ? a.V - first : p.piece;
+    const bool last = first + a.piece_classes == a.V;
     if (p.side == 256) launch_grad<4, 2, 2, 4>(a, stream);
     else if (p.side == 128) launch_grad<2, 1, 2, 4>(a, stream);
     else launch_grad<1, 1, 2, 2>(a, stream);
-    e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    const uint16_t* weight = a.half_weight + (int64_t)first * a.D;
+    Product tokens{}, weight{};
     if (a.grad_tokens) {
       // rows: packed rows; k: classes of the piece (g holds zeros up to a multiple of 8 behind them)
-      MatmulArgs m{};
-      m.A = a.g, m.lda = p.piece_ld, m.B = weight, m.ldb = a.D;
-      m.M = a.M, m.N = a.D, m.K = a.piece_classes, m.rows = a.count;
-      m.out = a.tokens_acc, m.parts = p.tokens_parts, m.accumulate = first > 0;
-      e = launch_matmul(m, MatmulKind::kHalfAlong, p.tokens_side, stream);
-      if (e != hipSuccess) return e;
+      tokens.A = a.g, tokens.lda = p.piece_ld;
+      tokens.B = a.half_weight + (int64_t)first * a.D, tokens.ldb = a.D, tokens.by_weight = true;
+      tokens.M = (int)a.M, tokens.N = a.D, tokens.K = a.piece_classes, tokens.rows = a.count;
+      tokens.parts = p.tokens_parts, tokens.acc = a.tokens_acc, tokens.accumulate = first > 0;
+      if (last) tokens.out = static_cast<uint16_t*>(a.grad_tokens), tokens.row_of = a.row_of;
     }
     if (a.grad_weight) {
-      MatmulArgs m{};
-      m.A = a.g, m.lda = p.piece_ld, m.B = a.half_tokens, m.ldb = a.D;
-      m.M = a.piece_classes, m.N = a.D, m.K = a.M, m.depth = a.count;
-      m.out = a.weight_acc, m.parts = p.weight_parts;
-      e = launch_matmul(m, MatmulKind::kHalfAcross, p.weight_side, stream);
-      if (e != hipSuccess) return e;
-      hipLaunchKernelGGL(class_weight_kernel, dim3(finish_blocks((int64_t)a.piece_classes * a.D)),
-                         dim3(kFinishThreads), 0, stream, a);
+      weight.A = a.g, weight.lda = p.piece_ld, weight.B = a.half_tokens, weight.ldb = a.D;
+      weight.M = a.piece_classes, weight.N = a.D, weight.K = (int)a.M, weight.depth = a.count;
+      weight.parts = p.weight_parts, weight.acc = a.weight_acc;
+      weight.out = static_cast<uint16_t*>(a.grad_weight) + (int64_t)first * a.D;
     }
-    if (a.grad_bias)
-      hipLaunchKernelGGL(class_bias_kernel, dim3((uint32_t)ceil_div(a.piece_classes, 64)), dim3(kFinishThreads), 0,
-                         stream, a);
+    if (a.grad_tokens || a.grad_weight) {
+      if (p.products_side == 256) launch_products<4, 2, 2, 4>(a, tokens, weight, stream);
+      else if (p.products_side == 128) launch_products<2, 1, 2, 4>(a, tokens, weight, stream);
+      else launch_products<1, 1, 2, 2>(a, tokens, weight, stream);
+    }
+    const uint32_t for_bias = a.grad_bias ? (uint32_t)ceil_div(a.piece_classes, 64) : 0;
+    const uint32_t for_weight =
+        a.grad_weight && p.weight_parts > 1 ? finish_blocks((int64_t)a.piece_classes * a.D) : 0;
+    const uint32_t for_tokens = a.grad_tokens && p.tokens_parts > 1 && last ? finish_blocks(a.M * a.D) : 0;
+    if (for_bias + for_weight + for_tokens > 0)
+      hipLaunchKernelGGL(class_finish_kernel, dim3(for_bias + for_weight + for_tokens), dim3(kFinishThreads), 0, stream, a,
+                         for_bias, for_weight);
     e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
-  if (a.grad_tokens)
-    hipLaunchKernelGGL(class_tokens_kernel, dim3(finish_blocks(a.M * a.D)), dim3(kFinishThreads), 0, stream, a);
-  return hipGetLastError();
+  return hipSuccess;
 }
 
 }  // namespace mae

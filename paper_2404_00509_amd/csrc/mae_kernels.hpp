@@ -298,15 +298,15 @@ hipError_t launch_matmul(const MatmulArgs& a, MatmulKind kind, int side, hipStre
 
 // ---- softmax cross entropy of a linear head ----------------------------------------------------------------
 struct ClassPlan {
-  int side;                       // of the tiles of logits
-  int stat_tiles, pack_rows, num_partials;
-  int piece, piece_ld;            // classes per piece of the gradient; row length of g
-  int tokens_side, tokens_parts;  // product for grad_tokens
-  int weight_side, weight_parts;  // product for grad_weight
+  int few;                            // the loss alone of few rows: nothing is packed
+  int side;                           // of the tiles of logits
+  int stat_tiles, pack_rows, row_blocks;
+  int piece, piece_ld;                // classes per piece of the gradient; row length of g
+  int products_side, tokens_parts, weight_parts;  // of the products for grad_tokens and grad_weight
+  int num_peaks, num_weight_peaks;    // workgroups of the first kernel; of them, those that look at the weight
   // places in the workspace
-  size_t count, slot_of, label_of, packed, stats, logit_sums, label_logit, row_max, row_inv, partials;
-  int num_peaks, num_weight_peaks;  // workgroups of the first kernel; of them, those that look at the weight
-  size_t peaks, half_tokens, half_weight, g, column_sums, tokens_acc, weight_acc;
+  size_t stats, logit_sums, label_logit, count, label_of, row_of, packed, partials;
+  size_t peaks, row_max, row_inv, half_tokens, half_weight, g, column_sums, tokens_acc, weight_acc;
   size_t bytes;
 };
 ClassPlan class_plan(int64_t M, int D, int V, bool grad);
@@ -324,25 +324,25 @@ struct ClassArgs {
   void* grad_weight;  // [V, D] bf16, nullable
   float* grad_bias;   // [V], nullable
   // workspace: rows whose label is a class, one after the other ("slots")
-  int32_t* count;      // their number
-  int32_t* slot_of;    // [M] slot of a row, -1: left out
+  int32_t* count;      // their number; null: every row has its slot (the labels are looked at by the last kernel)
   int32_t* label_of;   // [slot]
+  int32_t* row_of;     // [slot]
   uint16_t* packed;    // [slot][D]
   float* stats;        // [slot][stat_tiles][2] maximum, sum of exponentials
   float* logit_sums;   // [slot][stat_tiles], null without smoothing
   float* label_logit;  // [slot]
+  double* partials;    // [row_blocks] sums of losses
+  int32_t* peaks;      // [num_peaks] largest finite magnitudes as bf16 bits: tokens, then weight; null: no gradient
   float* row_max;      // [slot]
   float* row_inv;      // [slot] 1 / sum of exponentials under the maximum
-  double* partials;
-  int32_t* peaks;         // [num_peaks] largest finite magnitudes as bf16 bits: tokens, then weight; null: no gradient
   uint16_t* half_tokens;  // [slot][D] fp16, scaled by a power of two
   uint16_t* half_weight;  // [V][D]
   uint16_t* g;            // [slot][piece_ld] fp16, times 2^15
-  float* column_sums;  // [row tile][classes of the piece]
-  float* tokens_acc;   // [tokens_parts][M][D]
-  float* weight_acc;   // [weight_parts][classes of the piece][D]
+  float* column_sums;     // [row tile][classes of the piece]
+  float* tokens_acc;      // [tokens_parts][M][D]
+  float* weight_acc;      // [weight_parts][classes of the piece][D]
   // filled in by the launcher
-  int32_t pack_rows, stat_tiles, pack_blocks, num_peaks;
+  int32_t pack_rows, stat_tiles, pack_blocks, num_peaks, row_blocks;
   int32_t piece_first, piece_classes, piece_ld, grad_rows, tokens_parts, weight_parts;
 };
 hipError_t launch_class_loss(ClassArgs a, const ClassPlan& p, hipStream_t stream);
