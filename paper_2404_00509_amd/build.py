@@ -9,7 +9,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(_HERE, "csrc")
 SOURCES = ["api.hip", "api_train.hip", "mask_params.hip", "crop_patch.hip", "normpix_loss.hip",
            "patch_embed.hip", "three_aug.hip", "jpeg_decode.hip", "layer_norm.hip", "dropout.hip",
-           "matmul.hip", "class_loss.hip", "embed_grad.hip"]
+           "class_loss.hip", "embed_grad.hip"]
 OUT = os.path.join(_HERE, "libmae_hip.so")
 
 HIPCC_FLAGS = [

@@ -72,7 +72,7 @@ int validate_class(const mae_class_desc* d) {
   return MAE_OK;
 }
 
-constexpr int kMaxPosRows = 8192;  // counters of the rows' patch indices lie in LDS
+constexpr int kMaxPosRows = 8192;  // the work of grad_pos grows with it
 
 int validate_embed_grad(const mae_embed_desc* d) {
   const int rc = mae::validate_embed(d);
@@ -224,10 +224,15 @@ int mae_class_loss(const mae_class_desc* d, float* loss, float* row_loss, void* 
 
 size_t mae_patch_embed_grad_workspace_bytes(const mae_embed_desc* d) {
   if (validate_embed_grad(d) != MAE_OK) return 0;
-  const size_t plain = mae::embed_grad_plan(d->M, d->D, d->E, d->L, false).bytes;
-  if (!d->pos) return plain;
-  const size_t sorted = mae::embed_grad_plan(d->M, d->D, d->E, d->L, true).bytes;
-  return sorted > plain ? sorted : plain;
+  // the largest need of any set of outputs
+  size_t most = 0;
+  for (int weight = 0; weight < 2; ++weight)
+    for (int pos : {0, 1, d->pos ? d->L : 1}) {
+      if (!weight && !pos) continue;
+      const size_t n = mae::embed_grad_plan(d->M, d->E, weight ? d->D : 0, pos, d->D).bytes;
+      if (n > most) most = n;
+    }
+  return most;
 }
 
 int mae_patch_embed_grad(const mae_embed_desc* d, const void* grad_tokens, float* grad_weight, float* grad_bias,
@@ -240,25 +245,21 @@ int mae_patch_embed_grad(const mae_embed_desc* d, const void* grad_tokens, float
   if (!has_workspace(workspace, workspace_bytes, mae_patch_embed_grad_workspace_bytes(d))) return MAE_ERR_WORKSPACE;
   rc = have_device();
   if (rc != MAE_OK) return rc;
-  const bool by_index = grad_pos != nullptr;
-  const mae::EmbedGradPlan p = mae::embed_grad_plan(d->M, d->D, d->E, d->L, by_index);
-  char* ws = static_cast<char*>(workspace);
   mae::EmbedGradArgs a{};
   a.M = d->M;
   a.D = d->D;
   a.E = d->E;
-  a.L = d->L;
+  a.pos_columns = grad_pos ? d->L : grad_bias ? 1 : 0;
+  const mae::EmbedGradPlan p = mae::embed_grad_plan(d->M, d->E, grad_weight ? d->D : 0, a.pos_columns, d->D);
+  char* ws = static_cast<char*>(workspace);
   a.g = static_cast<const uint16_t*>(grad_tokens);
   a.visible = static_cast<const uint16_t*>(d->visible);
-  a.ids = d->ids_keep;
+  a.ids = grad_pos ? d->ids_keep : nullptr;
   a.grad_weight = grad_weight;
   a.grad_bias = grad_bias;
   a.grad_pos = grad_pos;
-  a.counts = reinterpret_cast<int32_t*>(ws + p.counts);
-  a.starts = reinterpret_cast<int32_t*>(ws + p.starts);
-  a.order = by_index ? reinterpret_cast<int32_t*>(ws + p.order) : nullptr;
-  a.pos_parts = reinterpret_cast<float*>(ws + p.pos_parts);
   a.weight_acc = reinterpret_cast<float*>(ws + p.weight_acc);
+  a.pos_acc = reinterpret_cast<float*>(ws + p.pos_acc);
   return mae::launch_embed_grad(a, p, reinterpret_cast<uint16_t*>(ws + p.padded),
                                 static_cast<hipStream_t>(hip_stream)) == hipSuccess
              ? MAE_OK

@@ -278,24 +278,6 @@ struct DropoutArgs {
 };
 hipError_t launch_dropout(const DropoutArgs& a, hipStream_t stream);
 
-// ---- products of bf16 or fp16 matrices into fp32 parts -----------------------------------------------------------
-// part s of out[s][m][n] = sum over its share of k of A(m, k) B[k][n], B with k as its row number
-struct MatmulArgs {
-  const uint16_t* A;  // "along": A[m][k]; otherwise A[k][m]
-  const uint16_t* B;  // B[k][n]
-  int64_t lda, ldb;   // values from row to row
-  int64_t M, K;
-  int32_t N, parts;
-  const int32_t* rows;   // nullable: only so many m (device memory)
-  const int32_t* depth;  // nullable: only so many k
-  float* out;
-  int32_t accumulate;  // added to what is there
-};
-int matmul_side(int64_t M, int N);                             // of the tiles
-int matmul_parts(int64_t M, int N, int64_t K, int side);       // k is split into
-enum class MatmulKind { kHalfAlong, kHalfAcross, kBf16Across };  // operands' type, how A lies
-hipError_t launch_matmul(const MatmulArgs& a, MatmulKind kind, int side, hipStream_t stream);
-
 // ---- softmax cross entropy of a linear head ----------------------------------------------------------------
 struct ClassPlan {
   int few;                            // the loss alone of few rows: nothing is packed
@@ -349,28 +331,25 @@ hipError_t launch_class_loss(ClassArgs a, const ClassPlan& p, hipStream_t stream
 
 // ---- gradients of the patch embedding --------------------------------------------------------------------
 struct EmbedGradPlan {
-  int ld;        // row length of g: E, or E rounded up to 8 in a copy
-  int last_row;  // the last row's products come from the joining kernel
-  int rows;      // rows of grad_pos that are summed (1: the bias alone)
-  int side, parts, chunk_rows, chunks, shares;
-  size_t padded, counts, starts, order, pos_parts, weight_acc, bytes;
+  int ld;     // row length of g: E, or E rounded up to 8 in a copy
+  int64_t K;  // rows that the product kernel takes: M, or M - 1
+  int side, parts;
+  size_t padded, weight_acc, pos_acc, bytes;
 };
-EmbedGradPlan embed_grad_plan(int64_t M, int D, int E, int L, bool by_index);
+// weight_columns: D, or 0 without grad_weight; pos_columns: L with grad_pos, 1 with grad_bias alone, 0 without both.
+EmbedGradPlan embed_grad_plan(int64_t M, int E, int weight_columns, int pos_columns, int D);
 struct EmbedGradArgs {
-  int64_t M;
-  int32_t D, E, L;
-  const uint16_t* g;        // [M, E] bf16
+  int64_t M, K;
+  int32_t D, E;
+  int32_t ld, parts, pos_columns;
+  const uint16_t* g;        // [M, ld] bf16
   const uint16_t* visible;  // [M, D] bf16
-  const int32_t* ids;       // [M]
+  const int32_t* ids;       // [M], null without grad_pos
   float* grad_weight;       // [E, D], nullable
   float* grad_bias;         // [E], nullable
-  float* grad_pos;          // [L, E], nullable
-  int32_t* counts;          // [chunks][L]
-  int32_t* starts;          // [L + 1]
-  int32_t* order;           // [M], null: no grad_pos, rows in their own order
-  float* pos_parts;         // [rows][shares][ld]
+  float* grad_pos;          // [pos_columns, E], nullable
   float* weight_acc;        // [parts][E][D]
-  int32_t ld, parts, shares, chunks, chunk_rows, last_row;
+  float* pos_acc;           // [parts][E][pos_columns]
 };
 hipError_t launch_embed_grad(EmbedGradArgs a, const EmbedGradPlan& p, uint16_t* padded, hipStream_t stream);
 

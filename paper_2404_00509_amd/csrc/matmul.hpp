@@ -118,6 +118,11 @@ struct Tile {
   static_assert(kSlots % kThreads == 0 && NL % 2 == 0, "halves of whole wave-wide loads");
   static_assert(3 * NL <= 63, "vmcnt range");
 
+  // what the chunk's place is XORed with in row k of an operand across k
+  template <int R>
+  __device__ static inline int swizzle(int k) {
+    return R >= 128 ? (k & 3) << 2 : ((k >> 1) & 1) << 2;
+  }
   // which chunk of its row slot `s` of an operand of R rows or columns holds, and that row
   template <int R, bool kAlong>
   __device__ static inline void slot_place(int s, int* row, int* chunk) {
@@ -127,7 +132,7 @@ struct Tile {
     } else {
       constexpr int kChunks = R / 8;
       *row = s / kChunks;
-      *chunk = (s % kChunks) ^ (R >= 128 ? (*row & 3) << 2 : ((*row >> 1) & 1) << 2);
+      *chunk = (s % kChunks) ^ swizzle<R>(*row);
     }
   }
 
@@ -195,10 +200,21 @@ struct Tile {
     });
   }
 
+  // A second operand that is not in memory: row k of it is 1 at column ids[k] - first and 0 elsewhere (ids null: at
+  // column 0), so that the product adds up the columns of A whose k has the same id.  ids outside [0, count) are
+  // clamped into it.
+  struct Ones {
+    const int32_t* ids;  // of this tile's first k
+    int first, count;
+  };
+
   // The tile's sums.  kAhead: slices of the ring that fill() has been called for already (0, 2 or 4); no
   // wavefront uses what the others' places hold any more.
-  template <int kAhead>
-  __device__ static inline void run(const Source& src, u32x4* lds, f32x16 (&acc)[TM][TN]) {
+  // kOnes: B is made in LDS: the ring's places 0 to 2 are A's, 3 and 4 hold B, zero but for 64 values that the first
+  // wavefront moves from slice to slice.
+  template <int kAhead, bool kOnes = false>
+  __device__ static inline void run(const Source& src, u32x4* lds, f32x16 (&acc)[TM][TN], Ones ones = {}) {
+    static_assert(!kOnes || (kAhead == 0 && !kAlongB && !kHalf), "bf16 ones, across k");
     const int lane = threadIdx.x % kWave;
     const int wave = uniform((int)threadIdx.x / kWave);
     const int wm = wave / WGN, wn = wave % WGN;
@@ -287,45 +303,95 @@ struct Tile {
       arrive(set ^ 1);
     };
 
-    fill<kAhead, 5>(src, lds);
-    // slice 0 has landed; of what was issued here the rest may be on its way
-    static_assert(kAhead == 0 || kAhead == 2 || kAhead == 4, "whole slices of both operands");
-    constexpr int kRest = kAhead == 4 ? 1 : 3;
-    if (nk > 2) __builtin_amdgcn_s_waitcnt(wait_vm(kRest * NL));
-    else if (nk > 1) __builtin_amdgcn_s_waitcnt(wait_vm((kRest - 1) * NL));
-    else __builtin_amdgcn_s_waitcnt(wait_vm(0));
-    __builtin_amdgcn_s_barrier();
-    read_frags(0, 1, Tag<0>{}, 0);
+    // ones: byte of this lane's 1 in either place (-1: none), and the id of the slice after the last one made
+    int at_one[2] = {-1, -1}, next_id = 0;
+    auto load_id = [&](int it) {
+      const int k = it * kSlice + lane;
+      if (ones.ids) next_id = ones.ids[min(k, src.K - 1)];
+    };
+    auto make_ones = [&](int it) {  // (next_id is that of slice `it`)
+      if (wave != 0) return;
+      char* place = reinterpret_cast<char*>(lds + (3 + (it & 1)) * kSlots);
+      const int old = (it & 1) ? at_one[1] : at_one[0];
+      if (old >= 0) *reinterpret_cast<uint16_t*>(place + old) = 0;
+      const int c = min(max(next_id, 0), ones.count - 1) - ones.first;
+      int at = -1;
+      if (it * kSlice + lane < src.K && c >= 0 && c < BN) {
+        at = lane * BN * 2 + (((c >> 3) ^ swizzle<BN>(lane)) * 16) + (c & 7) * 2;
+        *reinterpret_cast<uint16_t*>(place + at) = 0x3F80;
+      }
+      if (it & 1) at_one[1] = at;
+      else at_one[0] = at;
+      if (it + 1 < nk) load_id(it + 1);
+    };
+
+    if constexpr (kOnes) {
+      unroll<3>([&](auto n) {
+        if (decltype(n)::value < nk) issue<true>(src, lds, decltype(n)::value, decltype(n)::value, 0, NL);
+      });
+      for (int i = threadIdx.x; i < 2 * kSlots; i += kThreads) lds[3 * kSlots + i] = u32x4{0u, 0u, 0u, 0u};
+      load_id(0);
+      __syncthreads();
+      make_ones(0);
+      __syncthreads();  // (waits for the loads of all three slices as well)
+    } else {
+      fill<kAhead, 5>(src, lds);
+      // slice 0 has landed; of what was issued here the rest may be on its way
+      static_assert(kAhead == 0 || kAhead == 2 || kAhead == 4, "whole slices of both operands");
+      constexpr int kRest = kAhead == 4 ? 1 : 3;
+      if (nk > 2) __builtin_amdgcn_s_waitcnt(wait_vm(kRest * NL));
+      else if (nk > 1) __builtin_amdgcn_s_waitcnt(wait_vm((kRest - 1) * NL));
+      else __builtin_amdgcn_s_waitcnt(wait_vm(0));
+      __builtin_amdgcn_s_barrier();
+    }
+    read_frags(0, kOnes ? 3 : 1, Tag<0>{}, 0);
     arrive(0);
 
     // A slice is four sub-steps of 16 k; the fragments of a sub-step are read while the one before it is
     // multiplied, across slices too; the loads that refill the ring are spread over all four.
-    int pa = 0;  // place of A of this slice; B's is the next one
+    // Places of the ring: A and B of this slice, of the next one, and A of the one after it.
+    auto after = [](int place) { return place + 1 == kPlaces ? 0 : place + 1; };
+    int pa = 0, pb = kOnes ? 3 : 1;
     for (int it = 0; it + 1 < nk; ++it) {
-      const int pb = pa + 1 == kPlaces ? 0 : pa + 1;
-      const int na = pb + 1 == kPlaces ? 0 : pb + 1, nb = na + 1 == kPlaces ? 0 : na + 1;  // of the next slice
-      const int ma = nb + 1 == kPlaces ? 0 : nb + 1;                                       // A of the one after it
+      int na, nb, ma;
+      if constexpr (kOnes) {
+        na = pa == 2 ? 0 : pa + 1;
+        nb = 7 - pb;
+        ma = na == 2 ? 0 : na + 1;
+        make_ones(it + 1);
+      } else {
+        na = after(pb);
+        nb = after(na);
+        ma = after(nb);
+      }
       constexpr int kHalfNL = NL / 2;
+      const bool more = it + 2 < nk;
       step(0, pa, pb, Tag<1>{}, [&](int q0, int q1) {
-        if (it >= 1) issue<false>(src, lds, it + 1, nb, kHalfNL + q0, kHalfNL + q1);
+        if constexpr (kOnes) {
+          if (it >= 1 && more) issue<true>(src, lds, it + 2, ma, q0, q1);
+        } else {
+          if (it >= 1) issue<false>(src, lds, it + 1, nb, kHalfNL + q0, kHalfNL + q1);
+        }
       });
       step(1, pa, pb, Tag<2>{}, [&](int q0, int q1) {
-        if (it >= 1 && it + 2 < nk) issue<true>(src, lds, it + 2, ma, q0, q1);
+        if (it >= 1 && more) issue<true>(src, lds, it + 2, ma, q0 + (kOnes ? kHalfNL : 0), q1 + (kOnes ? kHalfNL : 0));
       });
       step(0, pa, pb, Tag<3>{}, [&](int q0, int q1) {
-        if (it >= 1 && it + 2 < nk) issue<true>(src, lds, it + 2, ma, kHalfNL + q0, kHalfNL + q1);
+        if constexpr (!kOnes)
+          if (it >= 1 && more) issue<true>(src, lds, it + 2, ma, kHalfNL + q0, kHalfNL + q1);
       });
       // the next slice has landed (the A behind it may be on its way) for all wavefronts, and all have read what
       // they need of this one
-      if (it + 2 < nk) __builtin_amdgcn_s_waitcnt(wait_vm(NL));
+      if (more) __builtin_amdgcn_s_waitcnt(wait_vm(NL));
       else __builtin_amdgcn_s_waitcnt(wait_vm(0));
       __builtin_amdgcn_s_barrier();
       step(1, na, nb, Tag<0>{}, [&](int q0, int q1) {  // (B of slice it + 2 goes where A of this one was)
-        if (it + 2 < nk) issue<false>(src, lds, it + 2, pa, q0, q1);
+        if constexpr (!kOnes)
+          if (more) issue<false>(src, lds, it + 2, pa, q0, q1);
       });
       pa = na;
+      pb = nb;
     }
-    const int pb = pa + 1 == kPlaces ? 0 : pa + 1;
     const int left = tail ? (tail + 15) / 16 : 4;  // sub-steps of the last slice that hold values
     if (left > 1) read_frags(pa, pb, Tag<1>{}, 1);
     multiply(0);
@@ -350,8 +416,7 @@ struct Tile {
   template <int R>
   __device__ static inline uint32_t across_at(int block, int g, int i) {
     const int k = (g >> 1) * 8 + (i >> 2);
-    const int swizzle = R >= 128 ? (k & 3) << 2 : ((k >> 1) & 1) << 2;
-    const int chunk = (block * 4 + (g & 1) * 2 + ((i & 3) >> 1)) ^ swizzle;
+    const int chunk = (block * 4 + (g & 1) * 2 + ((i & 3) >> 1)) ^ swizzle<R>(k);
     return (uint32_t)(k * R * 2 + chunk * 16 + (i & 1) * 8);
   }
   template <int R, bool kAlong, int ks, int r, int T, int N>
