@@ -224,15 +224,7 @@ int mae_class_loss(const mae_class_desc* d, float* loss, float* row_loss, void* 
 
 size_t mae_patch_embed_grad_workspace_bytes(const mae_embed_desc* d) {
   if (validate_embed_grad(d) != MAE_OK) return 0;
-  // the largest need of any set of outputs
-  size_t most = 0;
-  for (int weight = 0; weight < 2; ++weight)
-    for (int pos : {0, 1, d->pos ? d->L : 1}) {
-      if (!weight && !pos) continue;
-      const size_t n = mae::embed_grad_plan(d->M, d->E, weight ? d->D : 0, pos, d->D).bytes;
-      if (n > most) most = n;
-    }
-  return most;
+  return mae::embed_grad_plan(d->M, d->D, d->E, d->pos ? d->L : 1).bytes;
 }
 
 int mae_patch_embed_grad(const mae_embed_desc* d, const void* grad_tokens, float* grad_weight, float* grad_bias,
@@ -250,7 +242,7 @@ int mae_patch_embed_grad(const mae_embed_desc* d, const void* grad_tokens, float
   a.D = d->D;
   a.E = d->E;
   a.pos_columns = grad_pos ? d->L : grad_bias ? 1 : 0;
-  const mae::EmbedGradPlan p = mae::embed_grad_plan(d->M, d->E, grad_weight ? d->D : 0, a.pos_columns, d->D);
+  const mae::EmbedGradPlan p = mae::embed_grad_plan(d->M, d->D, d->E, d->pos ? d->L : 1);
   char* ws = static_cast<char*>(workspace);
   a.g = static_cast<const uint16_t*>(grad_tokens);
   a.visible = static_cast<const uint16_t*>(d->visible);

@@ -764,10 +764,12 @@ namespace {
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 size_t up256(size_t n) { return (n + 255) & ~size_t(255); }
 
-// Side of the tiles of logits.
+// Side of the tiles of logits: the largest of which there are enough.  Loss alone, us for 64 / 128 / 256: 2048 x 768 over
+// 1000 classes 21.9 / 24.5 / 36, 4096 28.5 / 27.6 / 41, 8192 43 / 36.4 / 43.5, 16384 68 / 54.4 / 50.0; 1024 x 1024
+// over 8192 42.6 / 34.2 / 39.8; 512 x 768 over 21,841 45 / 36.2 / 35.6; 2048 x 1024 over 32,003 228 / 166 / 134.
 int logits_side(int64_t M, int V) {
-  if (ceil_div(M, 128) * ceil_div(V, 128) < 128) return 64;
-  if (ceil_div(M, 256) * ceil_div(V, 256) < 512) return 128;
+  if (ceil_div(M, 128) * ceil_div(V, 128) < 192) return 64;
+  if (ceil_div(M, 256) * ceil_div(V, 256) < 256) return 128;
   return 256;
 }
 
@@ -781,11 +783,14 @@ int product_parts(int64_t M, int N, int64_t K, int side, int64_t slots) {
 
 }  // namespace
 
-// Side of the tiles of the two products of a piece.
+// Side of the tiles of the two products of a piece, the largest of which there are enough.  Whole calls, us for 64 / 128 /
+// 256: 512 x 768 over 1000 classes 43.8 / 47.0 / 60, 1024 44.1 / 48.3 / 61, 2048 59.1 / 60.3 / 70, 4096 75.8 / 69.4 / 78.5,
+// 16384 199 / 177 / 182; 128 x 1024 over 32,003 128 / 119 / 136, 512 x 768 over 21,841 149 / 137 / 137, 2048 x 1024 over
+// 32,003 714 / 598 / 555.
 static int products_side(int64_t M, int D, int V) {
-  if (M <= 64 || V <= 64) return 64;
-  const int64_t tiles = ceil_div(M, 256) * ceil_div(D, 256) + ceil_div(V, 256) * ceil_div(D, 256);
-  return tiles < 256 ? 128 : 256;
+  const auto tiles = [&](int side) { return (ceil_div(M, side) + ceil_div(V, side)) * ceil_div(D, side); };
+  if (M <= 64 || V <= 64 || tiles(128) < 128) return 64;
+  return M <= 256 || tiles(256) < 256 ? 128 : 256;
 }
 
 ClassPlan class_plan(int64_t M, int D, int V, bool grad) {
@@ -819,9 +824,10 @@ ClassPlan class_plan(int64_t M, int D, int V, bool grad) {
     if (p.piece > V) p.piece = V;
     p.piece_ld = (int)ceil_div(p.piece, 64) * 64;
     p.products_side = products_side(M, D, p.piece);
-    const int64_t slots = p.products_side == 256 ? 256 : p.products_side == 128 ? 256 : 512;
-    p.tokens_parts = product_parts(M, D, p.piece, p.products_side, slots);
-    p.weight_parts = product_parts(p.piece, D, M, p.products_side, slots);
+    // (the tiles for grad_weight alone fill the compute units: the others, in the same launch, are split less)
+    const bool many = ceil_div(p.piece, p.products_side) * ceil_div(D, p.products_side) >= 256;
+    p.tokens_parts = product_parts(M, D, p.piece, p.products_side, many ? 128 : 256);
+    p.weight_parts = product_parts(p.piece, D, M, p.products_side, 256);
     p.num_weight_peaks = (int)(ceil_div((int64_t)V * D / 8, kPackThreads * 4) < 1024
                                    ? ceil_div((int64_t)V * D / 8, kPackThreads * 4) : 1024);
     p.num_peaks = (int)ceil_div(M, p.pack_rows) + p.num_weight_peaks;

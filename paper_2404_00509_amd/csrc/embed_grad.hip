@@ -140,13 +140,18 @@ void launch_products(const EmbedGradArgs& a, uint32_t blocks, hipStream_t stream
 
 }  // namespace
 
-EmbedGradPlan embed_grad_plan(int64_t M, int E, int weight_columns, int pos_columns, int D) {
+EmbedGradPlan embed_grad_plan(int64_t M, int D, int E, int L) {
   EmbedGradPlan p{};
   p.ld = E % 4 == 0 ? E : (int)ceil_div(E, 8) * 8;
   p.K = p.ld % 8 != 0 || D % 8 != 0 ? M - 1 : M;
-  p.side = M <= 512 ? 64 : M <= 4096 ? 128 : 256;
-  const int64_t tiles = tiles_of(p.side, E, weight_columns, pos_columns);
-  int64_t parts = (p.side == 256 ? 256 : p.side == 128 ? 512 : 1024) / tiles;
+  // Side of the tiles by the number of products; as many parts as fill the compute units, of four slices at least.
+  // us for tiles of 64 / 128 / 256, 768 -> 768, 196 patches: 784 rows 14.4 / 19.5 / 31, 1568 17.4 / 21.3 / 32, 3136
+  // 23.4 / 24.0 / 33, 6272 30.0 / 26.3 / 37.4, 12544 44.8 / 35.4 / 43.2, 25088 73 / 54.7 / 55.2, 50176 130 / 93 / 83,
+  // 200704 - / 347 / 271; 192 -> 384, 100 patches: 50000 rows 30.6 / 28.3 / 38; 192 -> 192: 8192 rows 12.2 / 14.1 / 21
+  const int64_t work = M * E * (D + L);
+  p.side = work < 2300000000 ? 64 : work < 19000000000 ? 128 : 256;
+  const int64_t tiles = tiles_of(p.side, E, D, L);
+  int64_t parts = (p.side == 256 ? 256 : 512) / tiles;
   if (parts > ceil_div(p.K, kSlice) / 4) parts = ceil_div(p.K, kSlice) / 4;
   p.parts = (int)(parts < 1 ? 1 : parts);
   size_t at = 0;
@@ -156,8 +161,8 @@ EmbedGradPlan embed_grad_plan(int64_t M, int E, int weight_columns, int pos_colu
     return was;
   };
   p.padded = take(p.ld != E ? (size_t)M * p.ld * 2 : 0);
-  p.weight_acc = take((size_t)p.parts * E * weight_columns * 4);
-  p.pos_acc = take((size_t)p.parts * E * pos_columns * 4);
+  p.weight_acc = take((size_t)p.parts * E * D * 4);
+  p.pos_acc = take((size_t)p.parts * E * L * 4);
   p.bytes = at;
   return p;
 }

@@ -336,12 +336,13 @@ struct EmbedGradPlan {
   int side, parts;
   size_t padded, weight_acc, pos_acc, bytes;
 };
-// weight_columns: D, or 0 without grad_weight; pos_columns: L with grad_pos, 1 with grad_bias alone, 0 without both.
-EmbedGradPlan embed_grad_plan(int64_t M, int E, int weight_columns, int pos_columns, int D);
+// L: 1 without positional rows.  The plan does not depend on which of the gradients a call wants, nor do their bits.
+EmbedGradPlan embed_grad_plan(int64_t M, int D, int E, int L);
 struct EmbedGradArgs {
   int64_t M, K;
   int32_t D, E;
-  int32_t ld, parts, pos_columns;
+  int32_t ld, parts;
+  int32_t pos_columns;      // L with grad_pos, 1 with grad_bias alone, 0 without both
   const uint16_t* g;        // [M, ld] bf16
   const uint16_t* visible;  // [M, D] bf16
   const int32_t* ids;       // [M], null without grad_pos
