@@ -25,26 +25,40 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef f32x4 f32x4_a4 __attribute__((aligned(4)));
 typedef u32x2 u32x2_a2 __attribute__((aligned(2)));
 
-constexpr int kThreads = 256;
-
-// Four values, the first n of them where n < 4 (zeros behind).
+// Four values as they lie in memory.
 template <bool kBf16>
-__device__ inline f32x4 load4(const void* p, int64_t at, int n) {
-  f32x4 v = f32x4{0.f, 0.f, 0.f, 0.f};
-  if (n >= 4) {
-    if (kBf16) {
-      const u32x2 raw = *reinterpret_cast<const u32x2_a2*>(static_cast<const uint16_t*>(p) + at);
-      return f32x4{bf16_lo(raw.x), bf16_hi(raw.x), bf16_lo(raw.y), bf16_hi(raw.y)};
-    }
-    return *reinterpret_cast<const f32x4_a4*>(static_cast<const float*>(p) + at);
+struct Raw {
+  using Type = f32x4;
+};
+template <>
+struct Raw<true> {
+  using Type = u32x2;
+};
+
+// The first n (none, or 1 to 4) of four values, zeros behind.
+template <bool kBf16>
+__device__ inline typename Raw<kBf16>::Type load4(const void* p, int64_t at, int n) {
+  if constexpr (kBf16) {
+    const uint16_t* q = static_cast<const uint16_t*>(p) + at;
+    if (n >= 4) return *reinterpret_cast<const u32x2_a2*>(q);
+    u32x2 v = u32x2{0u, 0u};
+    if (n > 0) v.x = q[0];
+    if (n > 1) v.x |= (uint32_t)q[1] << 16;
+    if (n > 2) v.y = q[2];
+    return v;
+  } else {
+    const float* q = static_cast<const float*>(p) + at;
+    if (n >= 4) return *reinterpret_cast<const f32x4_a4*>(q);
+    f32x4 v = f32x4{0.f, 0.f, 0.f, 0.f};
+    if (n > 0) v.x = q[0];
+    if (n > 1) v.y = q[1];
+    if (n > 2) v.z = q[2];
+    return v;
   }
-#pragma unroll
-  for (int j = 0; j < 3; ++j)
-    if (j < n)
-      v[j] = kBf16 ? __uint_as_float((uint32_t)static_cast<const uint16_t*>(p)[at + j] << 16)
-                   : static_cast<const float*>(p)[at + j];
-  return v;
 }
+__device__ inline f32x4 values(f32x4 v) { return v; }
+__device__ inline f32x4 values(u32x2 v) { return f32x4{bf16_lo(v.x), bf16_hi(v.x), bf16_lo(v.y), bf16_hi(v.y)}; }
+
 template <bool kBf16>
 __device__ inline void store4(void* p, int64_t at, f32x4 v, int n) {
   if (n >= 4) {
@@ -65,11 +79,20 @@ __device__ inline void store4(void* p, int64_t at, f32x4 v, int n) {
 
 __device__ inline float sum4(f32x4 v) { return (v.x + v.y) + (v.z + v.w); }
 
+// v plus that of the lane `kBy` places further round in its group of 16: no trip through LDS, as shuffles take.
+template <int kBy>
+__device__ inline float add_rotated(float v) {
+  return v + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x120 | kBy, 0xF, 0xF, true));
+}
+__device__ inline float lane_value(float v, int lane) {
+  return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), lane));
+}
 // Sum over the kLanes lanes that hold a row; `slots`: 4 floats of LDS per use for rows of a workgroup.
 template <int kLanes>
 __device__ inline float row_sum(float v, float* slots) {
-#pragma unroll
-  for (int off = (kLanes < kWave ? kLanes : kWave) / 2; off > 0; off >>= 1) v += __shfl_xor(v, off, kWave);
+  v = add_rotated<1>(add_rotated<2>(add_rotated<4>(add_rotated<8>(v))));
+  if constexpr (kLanes >= kWave)
+    v = (lane_value(v, 0) + lane_value(v, 16)) + (lane_value(v, 32) + lane_value(v, 48));
   if constexpr (kLanes > kWave) {
     if (threadIdx.x % kWave == 0) slots[threadIdx.x / kWave] = v;
     __syncthreads();
@@ -78,10 +101,16 @@ __device__ inline float row_sum(float v, float* slots) {
   return v;
 }
 
+constexpr int kThreads = 256;
+// Rows that a group of lanes has in hand at a time, beside as many whose loads are on their way.
+template <int kLanes, int NV>
+constexpr int rows_at_once() { return kLanes <= kWave && NV <= 3 ? 2 : 1; }
+
 // NV: groups of four values per lane.
 template <int kLanes, int NV, bool kBf16In, bool kBf16Out>
 __global__ __launch_bounds__(kThreads) void layer_norm_kernel(NormArgs a) {
-  constexpr int kRows = kThreads / kLanes;  // rows of a workgroup at a time
+  constexpr int R = rows_at_once<kLanes, NV>();
+  constexpr int kRows = kThreads / kLanes * R;  // of a workgroup at a time
   __shared__ float slots[2][2][4];
   const int lane = threadIdx.x % kLanes;
   const int D = a.D;
@@ -91,51 +120,74 @@ __global__ __launch_bounds__(kThreads) void layer_norm_kernel(NormArgs a) {
 #pragma unroll
   for (int v = 0; v < NV; ++v) {
     const int c = 4 * (lane + v * kLanes);
-    n[v] = min(4, D - c);
+    n[v] = max(0, min(4, D - c));
     w[v] = f32x4{1.f, 1.f, 1.f, 1.f};
     b[v] = f32x4{0.f, 0.f, 0.f, 0.f};
-    if (a.weight && n[v] > 0) w[v] = load4<false>(a.weight, c, n[v]);
-    if (a.bias && n[v] > 0) b[v] = load4<false>(a.bias, c, n[v]);
+    if (a.weight) w[v] = load4<false>(a.weight, c, n[v]);
+    if (a.bias) b[v] = load4<false>(a.bias, c, n[v]);
   }
+  typename Raw<kBf16In>::Type next[R][NV];
+  const auto load = [&](int64_t row0) {
+#pragma unroll
+    for (int u = 0; u < R; ++u)
+#pragma unroll
+      for (int v = 0; v < NV; ++v)
+        next[u][v] = load4<kBf16In>(a.x, (row0 + u) * D + 4 * (lane + v * kLanes), row0 + u < a.M ? n[v] : 0);
+  };
+  int64_t row0 = (int64_t)blockIdx.x * kRows + (int)threadIdx.x / kLanes * R;
+  const int64_t step = (int64_t)gridDim.x * kRows;
+  load(row0);
   int turn = 0;
-  for (int64_t row0 = (int64_t)blockIdx.x * kRows; row0 < a.M; row0 += (int64_t)gridDim.x * kRows) {
-    const int64_t row = row0 + threadIdx.x / kLanes;
-    const bool live = row < a.M;
-    const int64_t at = row * D;
-    f32x4 x[NV];
-    float s = 0.f;
+  // (rows of a workgroup: all lanes of it take the same number of turns)
+  for (; row0 < a.M; row0 += step) {
+    f32x4 x[R][NV];
+    float s[R];
 #pragma unroll
-    for (int v = 0; v < NV; ++v) {
-      x[v] = f32x4{0.f, 0.f, 0.f, 0.f};
-      if (live && n[v] > 0) x[v] = load4<kBf16In>(a.x, at + 4 * (lane + v * kLanes), n[v]);
-      s += sum4(x[v]);
+    for (int u = 0; u < R; ++u) {
+      s[u] = 0.f;
+#pragma unroll
+      for (int v = 0; v < NV; ++v) {
+        x[u][v] = values(next[u][v]);
+        s[u] += sum4(x[u][v]);
+      }
     }
-    const float mean = row_sum<kLanes>(s, slots[turn][0]) / count;
-    float ss = 0.f;
+    load(row0 + step);
+    float mean[R], rstd[R];
 #pragma unroll
-    for (int v = 0; v < NV; ++v) {
+    for (int u = 0; u < R; ++u) mean[u] = row_sum<kLanes>(s[u], slots[turn][0]) / count;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) x[v][j] = j < n[v] ? x[v][j] - mean : 0.f;
-      ss += (x[v].x * x[v].x + x[v].y * x[v].y) + (x[v].z * x[v].z + x[v].w * x[v].w);
+    for (int u = 0; u < R; ++u) {
+      s[u] = 0.f;
+#pragma unroll
+      for (int v = 0; v < NV; ++v) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[u][v][j] = j < n[v] ? x[u][v][j] - mean[u] : 0.f;
+        s[u] += sum4(x[u][v] * x[u][v]);
+      }
     }
-    const float rstd = 1.0f / sqrtf(row_sum<kLanes>(ss, slots[turn][1]) / count + a.eps);
+#pragma unroll
+    for (int u = 0; u < R; ++u) rstd[u] = 1.0f / sqrtf(row_sum<kLanes>(s[u], slots[turn][1]) / count + a.eps);
     turn ^= 1;
-    if (!live) continue;
-    if (lane == 0) {
-      if (a.mean_out) a.mean_out[row] = mean;
-      if (a.rstd_out) a.rstd_out[row] = rstd;
-    }
 #pragma unroll
-    for (int v = 0; v < NV; ++v)
-      if (n[v] > 0)
-        store4<kBf16Out>(a.y, at + 4 * (lane + v * kLanes), x[v] * rstd * w[v] + b[v], n[v]);
+    for (int u = 0; u < R; ++u) {
+      const int64_t row = row0 + u;
+      if (row >= a.M) continue;
+      if (lane == 0) {
+        if (a.mean_out) a.mean_out[row] = mean[u];
+        if (a.rstd_out) a.rstd_out[row] = rstd[u];
+      }
+#pragma unroll
+      for (int v = 0; v < NV; ++v)
+        if (n[v] > 0) store4<kBf16Out>(a.y, row * D + 4 * (lane + v * kLanes), x[u][v] * rstd[u] * w[v] + b[v], n[v]);
+    }
   }
 }
 
 // kParams: the gradients of weight and bias are wanted.
 template <int kLanes, int NV, bool kBf16In, bool kBf16Out, bool kParams>
 __global__ __launch_bounds__(kThreads) void layer_norm_grad_kernel(NormArgs a) {
-  constexpr int kRows = kThreads / kLanes;
+  constexpr int R = rows_at_once<kLanes, NV>();
+  constexpr int kRows = kThreads / kLanes * R;
   __shared__ float slots[2][2][4];
   __shared__ f32x4 shares[kParams && kLanes <= kWave ? kThreads / kWave : 1][2 * kWave];
   const int lane = threadIdx.x % kLanes;
@@ -146,47 +198,71 @@ __global__ __launch_bounds__(kThreads) void layer_norm_grad_kernel(NormArgs a) {
 #pragma unroll
   for (int v = 0; v < NV; ++v) {
     const int c = 4 * (lane + v * kLanes);
-    n[v] = min(4, D - c);
+    n[v] = max(0, min(4, D - c));
     w[v] = f32x4{1.f, 1.f, 1.f, 1.f};
     gw[v] = gb[v] = f32x4{0.f, 0.f, 0.f, 0.f};
-    if (a.weight && n[v] > 0) w[v] = load4<false>(a.weight, c, n[v]);
+    if (a.weight) w[v] = load4<false>(a.weight, c, n[v]);
   }
+  typename Raw<kBf16In>::Type next_x[R][NV];
+  typename Raw<kBf16Out>::Type next_g[R][NV];
+  float next_mean[R], next_rstd[R];
+  const auto load = [&](int64_t row0) {
+#pragma unroll
+    for (int u = 0; u < R; ++u) {
+      const bool live = row0 + u < a.M;
+      next_mean[u] = live ? a.mean[row0 + u] : 0.f;
+      next_rstd[u] = live ? a.rstd[row0 + u] : 0.f;
+#pragma unroll
+      for (int v = 0; v < NV; ++v) {
+        const int64_t at = (row0 + u) * D + 4 * (lane + v * kLanes);
+        next_x[u][v] = load4<kBf16In>(a.x, at, live ? n[v] : 0);
+        next_g[u][v] = load4<kBf16Out>(a.grad_y, at, live ? n[v] : 0);
+      }
+    }
+  };
+  int64_t row0 = (int64_t)blockIdx.x * kRows + (int)threadIdx.x / kLanes * R;
+  const int64_t step = (int64_t)gridDim.x * kRows;
+  load(row0);
   int turn = 0;
-  for (int64_t row0 = (int64_t)blockIdx.x * kRows; row0 < a.M; row0 += (int64_t)gridDim.x * kRows) {
-    const int64_t row = row0 + threadIdx.x / kLanes;
-    const bool live = row < a.M;
-    const int64_t at = row * D;
-    const float mean = live ? a.mean[row] : 0.f, rstd = live ? a.rstd[row] : 0.f;
-    f32x4 h[NV], g[NV];
-    float s = 0.f, sh = 0.f;
+  for (; row0 < a.M; row0 += step) {
+    f32x4 h[R][NV], g[R][NV];
+    float rstd[R], s[R], sh[R];
 #pragma unroll
-    for (int v = 0; v < NV; ++v) {
-      h[v] = g[v] = f32x4{0.f, 0.f, 0.f, 0.f};
-      if (live && n[v] > 0) {
-        const int64_t e = at + 4 * (lane + v * kLanes);
-        h[v] = load4<kBf16In>(a.x, e, n[v]);
-        g[v] = load4<kBf16Out>(a.grad_y, e, n[v]);
+    for (int u = 0; u < R; ++u) {
+      rstd[u] = next_rstd[u];
+      s[u] = sh[u] = 0.f;
+#pragma unroll
+      for (int v = 0; v < NV; ++v) {
+        h[u][v] = (values(next_x[u][v]) - next_mean[u]) * rstd[u];
+        g[u][v] = values(next_g[u][v]);
+        if (kParams) {  // (values that do not exist have a zero gradient)
+          gw[v] += g[u][v] * h[u][v];
+          gb[v] += g[u][v];
+        }
+        g[u][v] *= w[v];
+        s[u] += sum4(g[u][v]);
+        sh[u] += sum4(g[u][v] * h[u][v]);
       }
     }
+    load(row0 + step);
+    float mg[R], mgh[R];
 #pragma unroll
-    for (int v = 0; v < NV; ++v) {
-      h[v] = (h[v] - mean) * rstd;
-      if (kParams) {  // (groups' values that do not exist hold a zero gradient)
-        gw[v] += g[v] * h[v];
-        gb[v] += g[v];
-      }
-      g[v] *= w[v];
-      s += sum4(g[v]);
-      sh += sum4(g[v] * h[v]);
+    for (int u = 0; u < R; ++u) {
+      mg[u] = row_sum<kLanes>(s[u], slots[turn][0]) / count;
+      mgh[u] = row_sum<kLanes>(sh[u], slots[turn][1]) / count;
     }
-    const float mg = row_sum<kLanes>(s, slots[turn][0]) / count;
-    const float mgh = row_sum<kLanes>(sh, slots[turn][1]) / count;
     turn ^= 1;
-    if (!live || !a.grad_x) continue;
+    if (!a.grad_x) continue;
 #pragma unroll
-    for (int v = 0; v < NV; ++v)
-      if (n[v] > 0)
-        store4<kBf16In>(a.grad_x, at + 4 * (lane + v * kLanes), (g[v] - mg - h[v] * mgh) * rstd, n[v]);
+    for (int u = 0; u < R; ++u) {
+      const int64_t row = row0 + u;
+      if (row >= a.M) continue;
+#pragma unroll
+      for (int v = 0; v < NV; ++v)
+        if (n[v] > 0)
+          store4<kBf16In>(a.grad_x, row * D + 4 * (lane + v * kLanes), (g[u][v] - mg[u] - h[u][v] * mgh[u]) * rstd[u],
+                          n[v]);
+    }
   }
   if constexpr (kParams) {
     // the workgroup's sums: [gridDim.x][2][D rounded up to 4]
@@ -227,18 +303,27 @@ __global__ __launch_bounds__(kThreads) void layer_norm_grad_kernel(NormArgs a) {
   }
 }
 
-// Sum of the workgroups' shares: 16 columns by 16 lanes each.
-__global__ __launch_bounds__(kThreads) void layer_norm_params_kernel(NormArgs a) {
-  __shared__ double part[16][17];
-  const int col = threadIdx.x % 16, r = threadIdx.x / 16;
-  const int c = blockIdx.x * 16 + col;  // of the 2 * padded columns
+// Sum of the workgroups' shares: 32 columns by 32 lanes each, sixteen loads in flight per lane.
+constexpr int kJoinThreads = 1024, kJoinColumns = 32, kJoinRows = kJoinThreads / kJoinColumns;
+__global__ __launch_bounds__(kJoinThreads) void layer_norm_params_kernel(NormArgs a) {
+  __shared__ double part[kJoinRows][kJoinColumns + 1];
+  const int col = threadIdx.x % kJoinColumns, r = threadIdx.x / kJoinColumns;
+  const int c = blockIdx.x * kJoinColumns + col, columns = 2 * a.padded;
+  const float* from = a.partials + min(c, columns - 1);
   double s = 0.0;
-  if (c < 2 * a.padded)
-    for (int p = r; p < a.num_partials; p += 16) s += (double)a.partials[(int64_t)p * 2 * a.padded + c];
+  constexpr int kBatch = 16;
+  for (int p0 = r; p0 < a.num_partials; p0 += kJoinRows * kBatch) {
+    float v[kBatch];
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k)
+      v[k] = from[(int64_t)min(p0 + kJoinRows * k, a.num_partials - 1) * columns];
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k) s += p0 + kJoinRows * k < a.num_partials ? (double)v[k] : 0.0;
+  }
   part[r][col] = s;
   __syncthreads();
-  if (r == 0 && c < 2 * a.padded) {
-    for (int k = 1; k < 16; ++k) s += part[k][col];
+  if (r == 0 && c < columns) {
+    for (int k = 1; k < kJoinRows; ++k) s += part[k][col];
     const int d = c < a.padded ? c : c - a.padded;
     float* out = c < a.padded ? a.grad_weight : a.grad_bias;
     if (out && d < a.D) out[d] = (float)s;
@@ -307,7 +392,7 @@ void launch_sized(const NormArgs& a, int blocks, bool grad, hipStream_t stream) 
 }
 
 int norm_blocks(int64_t M, int D, int most) {
-  const int rows = kThreads / norm_lanes(D);
+  const int rows = kThreads / norm_lanes(D) * (D <= 768 ? 2 : 1);  // rows_at_once
   const int64_t blocks = (M + rows - 1) / rows;
   return (int)(blocks < most ? blocks : most);
 }
@@ -325,7 +410,8 @@ hipError_t launch_layer_norm_grad(const NormArgs& a, hipStream_t stream) {
   launch_sized(a, norm_blocks(a.M, a.D, 1024), true, stream);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !a.partials) return e;
-  hipLaunchKernelGGL(layer_norm_params_kernel, dim3((2 * a.padded + 15) / 16), dim3(kThreads), 0, stream, a);
+  hipLaunchKernelGGL(layer_norm_params_kernel, dim3((2 * a.padded + kJoinColumns - 1) / kJoinColumns),
+                     dim3(kJoinThreads), 0, stream, a);
   return hipGetLastError();
 }
 
