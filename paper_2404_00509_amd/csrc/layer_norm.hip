@@ -359,7 +359,7 @@ void launch_backward(const NormArgs& a, int blocks, hipStream_t stream) {
 }
 
 // lanes per row
-int norm_lanes(int D) { return D <= 64 ? 16 : D <= 2048 ? 64 : 256; }
+int norm_lanes(int D) { return D <= 384 ? 16 : D <= 2048 ? 64 : 256; }
 
 template <int kLanes, int NV>
 void launch_either(const NormArgs& a, int blocks, bool grad, hipStream_t stream) {
@@ -370,10 +370,17 @@ void launch_either(const NormArgs& a, int blocks, bool grad, hipStream_t stream)
 
 void launch_sized(const NormArgs& a, int blocks, bool grad, hipStream_t stream) {
   const int groups = (a.D + 3) / 4;
-  if (a.D <= 64) return launch_either<16, 1>(a, blocks, grad, stream);
+  if (a.D <= 384) {
+    switch ((groups + 15) / 16) {
+      case 1: return launch_either<16, 1>(a, blocks, grad, stream);
+      case 2: return launch_either<16, 2>(a, blocks, grad, stream);
+      case 3: return launch_either<16, 3>(a, blocks, grad, stream);
+      case 4: return launch_either<16, 4>(a, blocks, grad, stream);
+      default: return launch_either<16, 6>(a, blocks, grad, stream);
+    }
+  }
   if (a.D <= 2048) {
     switch ((groups + 63) / 64) {
-      case 1: return launch_either<64, 1>(a, blocks, grad, stream);
       case 2: return launch_either<64, 2>(a, blocks, grad, stream);
       case 3: return launch_either<64, 3>(a, blocks, grad, stream);
       case 4: return launch_either<64, 4>(a, blocks, grad, stream);
@@ -392,7 +399,7 @@ void launch_sized(const NormArgs& a, int blocks, bool grad, hipStream_t stream) 
 }
 
 int norm_blocks(int64_t M, int D, int most) {
-  const int rows = kThreads / norm_lanes(D) * (D <= 768 ? 2 : 1);  // rows_at_once
+  const int rows = kThreads / norm_lanes(D) * ((D + 3) / 4 <= 3 * norm_lanes(D) && norm_lanes(D) <= kWave ? 2 : 1);  // rows_at_once
   const int64_t blocks = (M + rows - 1) / rows;
   return (int)(blocks < most ? blocks : most);
 }
