@@ -512,13 +512,21 @@ def _torch_dtype(dtype):
 
 
 def _one_device(*tensors, stream=None):
-    """Kernels run on the current device: every tensor (and the stream) has to belong to it."""
+    """Kernels run on the current device: every tensor, descriptor and the stream have to belong to it."""
     here = torch.cuda.current_device()
     for t in tensors:
         if t is not None and t.device.index != here:
             raise ValueError(f"tensor on {t.device}, but the current device is cuda:{here}")
     if stream is not None and stream.device.index != here:
         raise ValueError(f"stream of {stream.device}, but the current device is cuda:{here}")
+
+
+def _device_of(*tensors):
+    """The one device of a descriptor's tensors."""
+    devices = {t.device for t in tensors if t is not None}
+    if len(devices) > 1:
+        raise ValueError(f"tensors on different devices: {sorted(map(str, devices))}")
+    return devices.pop()
 
 
 def _bytes_of(t):
@@ -560,13 +568,14 @@ def make_dropout_desc(x, residual=None, *, p, rows_per_draw=0, seed=0, batch_ind
     d.p, d.rows_per_draw = p, rows_per_draw
     d.seed, d.batch_index, d.layer, d.row_base = seed, batch_index, layer, row_base
     d.tensors = (x, residual)
+    d.device = _device_of(x, residual)
     return d
 
 
 def mae_dropout(desc: MaeDropoutDesc, y, stream=None) -> None:
     """y = dropped x + residual.  Backward: the same keys with x = the gradient, no residual."""
     _check(y, "y", _torch_dtype(desc.dtype), numel=desc.M * desc.D)
-    _one_device(y, *desc.tensors, stream=stream)
+    _one_device(y, desc, stream=stream)
     rc = load().mae_dropout(C.byref(desc), _ptr(y), _stream(stream))
     if rc != MAE_OK:
         raise MaeError(rc, "mae_dropout")
@@ -586,6 +595,7 @@ def make_norm_desc(x, weight=None, bias=None, *, eps=1e-6, y_dtype=None) -> MaeN
     d.x_dtype = _mae_dtype(x)
     d.y_dtype = d.x_dtype if y_dtype is None else y_dtype
     d.tensors = (x, weight, bias)
+    d.device = _device_of(x, weight, bias)
     return d
 
 
@@ -593,7 +603,7 @@ def mae_layer_norm(desc: MaeNormDesc, y, mean=None, rstd=None, stream=None) -> N
     _check(y, "y", _torch_dtype(desc.y_dtype), numel=desc.M * desc.D)
     _check(mean, "mean", torch.float32, numel=desc.M, optional=True)
     _check(rstd, "rstd", torch.float32, numel=desc.M, optional=True)
-    _one_device(y, mean, rstd, *desc.tensors, stream=stream)
+    _one_device(y, mean, rstd, desc, stream=stream)
     rc = load().mae_layer_norm(C.byref(desc), _ptr(y), _ptr(mean), _ptr(rstd), _stream(stream))
     if rc != MAE_OK:
         raise MaeError(rc, "mae_layer_norm")
@@ -613,8 +623,7 @@ def mae_layer_norm_grad(desc: MaeNormDesc, grad_y, mean, rstd, grad_x=None, grad
     _check(grad_weight, "grad_weight", torch.float32, numel=desc.D, optional=True)
     _check(grad_bias, "grad_bias", torch.float32, numel=desc.D, optional=True)
     _check(workspace, "workspace", optional=True)
-    _one_device(grad_y, mean, rstd, grad_x, grad_weight, grad_bias, workspace, *desc.tensors,
-                stream=stream)
+    _one_device(grad_y, mean, rstd, grad_x, grad_weight, grad_bias, workspace, desc, stream=stream)
     rc = load().mae_layer_norm_grad(C.byref(desc), _ptr(grad_y), _ptr(mean), _ptr(rstd),
                                     _ptr(grad_x), _ptr(grad_weight), _ptr(grad_bias),
                                     _ptr(workspace), _bytes_of(workspace), _stream(stream))
@@ -641,6 +650,7 @@ def make_class_desc(tokens, labels, weight, bias=None, *, smoothing=0.0,
     d.bias, d.labels = _ptr(bias), labels.data_ptr()
     d.smoothing, d.grad_scale = smoothing, grad_scale
     d.tensors = (tokens, labels, weight, bias)
+    d.device = _device_of(tokens, labels, weight, bias)
     return d
 
 
@@ -656,8 +666,7 @@ def mae_class_loss(desc: MaeClassDesc, loss, row_loss=None, grad_tokens=None, gr
     _check(grad_weight, "grad_weight", torch.bfloat16, numel=desc.V * desc.D, optional=True)
     _check(grad_bias, "grad_bias", torch.float32, numel=desc.V, optional=True)
     _check(workspace, "workspace", optional=True)
-    _one_device(loss, row_loss, grad_tokens, grad_weight, grad_bias, workspace, *desc.tensors,
-                stream=stream)
+    _one_device(loss, row_loss, grad_tokens, grad_weight, grad_bias, workspace, desc, stream=stream)
     rc = load().mae_class_loss(C.byref(desc), _ptr(loss), _ptr(row_loss), _ptr(grad_tokens),
                                _ptr(grad_weight), _ptr(grad_bias), _ptr(workspace),
                                _bytes_of(workspace), _stream(stream))

@@ -351,24 +351,42 @@ __global__ __launch_bounds__(64 * WGM * WGN) void class_stats_kernel(ClassArgs a
 // One row by one wavefront: its loss; maximum and 1 / sum to memory.
 __device__ inline float join_row(const ClassArgs& a, int64_t slot, int lane) {
   const f32x2* st = reinterpret_cast<const f32x2*>(a.stats) + slot * a.stat_tiles;
+  const float own = a.label_logit[slot];
   float m = kNegInf, s = 0.f, sl = 0.f;
-  for (int t = lane; t < a.stat_tiles; t += kWave) m = fmaxf(m, st[t].x);
+  constexpr int kBatch = 8;  // loads in flight
+  for (int t0 = lane; t0 < a.stat_tiles; t0 += kBatch * kWave) {
+    f32x2 p[kBatch];
+    float top = m;
 #pragma unroll
-  for (int off = kWave / 2; off > 0; off >>= 1) m = fmaxf(m, __shfl_xor(m, off, kWave));
-  for (int t = lane; t < a.stat_tiles; t += kWave) {
-    const f32x2 p = st[t];
-    s += p.x == kNegInf ? p.y : p.y * exp_neg(p.x - m);
-    if (a.logit_sums) sl += a.logit_sums[slot * a.stat_tiles + t];
+    for (int k = 0; k < kBatch; ++k) {
+      p[k] = st[min(t0 + k * kWave, a.stat_tiles - 1)];
+      if (t0 + k * kWave >= a.stat_tiles) p[k] = f32x2{kNegInf, 0.f};
+      top = fmaxf(top, p[k].x);
+    }
+    if (a.logit_sums) {
+#pragma unroll
+      for (int k = 0; k < kBatch; ++k)
+        if (t0 + k * kWave < a.stat_tiles) sl += a.logit_sums[slot * a.stat_tiles + t0 + k * kWave];
+    }
+    // (-inf: nothing under it, or a NaN that reaches the sum)
+    s = m == kNegInf ? s : s * exp_neg(m - top);
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k) s += p[k].x == kNegInf ? p[k].y : p[k].y * exp_neg(p[k].x - top);
+    m = top;
   }
+  float top = m;
+#pragma unroll
+  for (int off = kWave / 2; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor(top, off, kWave));
+  s = m == kNegInf ? s : s * exp_neg(m - top);
 #pragma unroll
   for (int off = kWave / 2; off > 0; off >>= 1) {
     s += __shfl_xor(s, off, kWave);
     sl += __shfl_xor(sl, off, kWave);
   }
-  float v = (m + logf(s)) - (1.0f - a.smoothing) * a.label_logit[slot];
+  float v = (top + logf(s)) - (1.0f - a.smoothing) * own;
   if (a.logit_sums) v -= a.smoothing * (sl / (float)a.V);
   if (lane == 0 && a.peaks) {
-    a.row_max[slot] = m;
+    a.row_max[slot] = top;
     a.row_inv[slot] = 1.0f / s;
   }
   return v;
@@ -430,25 +448,29 @@ __global__ __launch_bounds__(kRowThreads) void class_loss_kernel(ClassArgs a) {
 // The rows of a call that did not pack any: one workgroup.
 constexpr int kFewThreads = 1024, kFewRows = 64;
 __global__ __launch_bounds__(kFewThreads) void class_few_rows_kernel(ClassArgs a) {
-  __shared__ double losses[kFewRows];
+  __shared__ float losses[kFewRows];
+  __shared__ int32_t in_rows[kFewRows];
   const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-  int n = 0;
-  for (int64_t row = wave; row < a.M; row += kFewThreads / kWave) {
+  for (int row = wave; row < (int)a.M; row += kFewThreads / kWave) {
     const bool in = (uint32_t)a.labels[row] < (uint32_t)a.V;
     const float v = in ? join_row(a, row, lane) : 0.f;
     if (lane == 0) {
-      losses[row] = (double)v;
+      losses[row] = v;
+      in_rows[row] = in ? 1 : 0;
       if (a.row_loss) a.row_loss[row] = v;
     }
   }
   __syncthreads();
-  if (threadIdx.x > 0) return;
-  double s = 0.0;
-  for (int64_t row = 0; row < a.M; ++row) {
-    s += losses[row];
-    n += (uint32_t)a.labels[row] < (uint32_t)a.V ? 1 : 0;
+  if (wave > 0) return;
+  static_assert(kFewRows == kWave, "a lane per row");
+  double s = lane < (int)a.M ? (double)losses[lane] : 0.0;
+  int n = lane < (int)a.M ? in_rows[lane] : 0;
+#pragma unroll
+  for (int off = kWave / 2; off > 0; off >>= 1) {
+    s += __shfl_xor(s, off, kWave);
+    n += __shfl_xor(n, off, kWave);
   }
-  *a.loss = n > 0 ? (float)(s / (double)n) : 0.f;
+  if (lane == 0) *a.loss = n > 0 ? (float)(s / (double)n) : 0.f;
 }
 
 // ---- the gradient of the logits, one piece of the classes -------------------------------------------------
@@ -768,8 +790,8 @@ size_t up256(size_t n) { return (n + 255) & ~size_t(255); }
 // 1000 classes 21.9 / 24.5 / 36, 4096 28.5 / 27.6 / 41, 8192 43 / 36.4 / 43.5, 16384 68 / 54.4 / 50.0; 1024 x 1024
 // over 8192 42.6 / 34.2 / 39.8; 512 x 768 over 21,841 45 / 36.2 / 35.6; 2048 x 1024 over 32,003 228 / 166 / 134.
 int logits_side(int64_t M, int V) {
-  if (ceil_div(M, 128) * ceil_div(V, 128) < 192) return 64;
-  if (ceil_div(M, 256) * ceil_div(V, 256) < 256) return 128;
+  if (M <= 64 || ceil_div(M, 128) * ceil_div(V, 128) < 192) return 64;
+  if (M <= 256 || ceil_div(M, 256) * ceil_div(V, 256) < 256) return 128;
   return 256;
 }
 
