@@ -5,13 +5,15 @@
 //   grad_x = rstd (g - mean(g) - h mean(g h)) with g = grad_y w
 //   grad_w = sum over rows of grad_y h;  grad_b = sum over rows of grad_y
 //
-// Bound by HBM: every value is read once and written once.  A row lies in the registers of 16 lanes
-// (up to 64 values), of a wavefront (up to 2048) or of a workgroup (up to 8192), four neighbouring
-// values per lane and step, so that mean and variance take two passes over registers instead of memory:
-// no difference of two large sums, as one pass with sums of squares would have.  A
-// wavefront takes rows in turn and keeps weight, bias and its share of their gradients in
-// registers; the shares of a workgroup are added through LDS, those of the workgroups by a second
-// kernel in a fixed order, in double precision, so results do not depend on scheduling.
+// Bound by HBM: every value is read once and written once.  A row lies in the registers of 16 lanes (up to 384 values), a
+// wavefront (1536) or a workgroup of 256 (6144) or 512 lanes, four neighbouring values per lane and step, so that mean and
+// variance take two passes over registers instead of memory: no difference of two large sums, as one pass with sums of
+// squares would have.  A group of lanes takes rows in turn, up to two at once, with the loads of the next ones on their way, and keeps
+// weight, bias and its share of their gradients in registers; sums over lanes go through DPP moves, not LDS.  The
+// shares of a workgroup are added through LDS, those of the workgroups by a second kernel in a fixed order, in double
+// precision, so results do not depend on scheduling.
+// 204,800 x 768 in bf16: forward 122 us (630 MB, 5.2 TB/s; 215 us without the loads ahead and with shuffles through LDS),
+// backward 172 + 6 us (945 MB, 5.3 TB/s); a copy of several GB runs at 4.7 TB/s on this card.
 #include "mae_device.hpp"
 #include "mae_kernels.hpp"
 
@@ -87,7 +89,8 @@ __device__ inline float add_rotated(float v) {
 __device__ inline float lane_value(float v, int lane) {
   return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), lane));
 }
-// Sum over the kLanes lanes that hold a row; `slots`: 4 floats of LDS per use for rows of a workgroup.
+// Sum over the kLanes lanes that hold a row; `slots`: kSlots floats of LDS per use for rows of a workgroup.
+constexpr int kSlots = 8;
 template <int kLanes>
 __device__ inline float row_sum(float v, float* slots) {
   v = add_rotated<1>(add_rotated<2>(add_rotated<4>(add_rotated<8>(v))));
@@ -97,21 +100,25 @@ __device__ inline float row_sum(float v, float* slots) {
     if (threadIdx.x % kWave == 0) slots[threadIdx.x / kWave] = v;
     __syncthreads();
     v = (slots[0] + slots[1]) + (slots[2] + slots[3]);
+    if constexpr (kLanes > 4 * kWave) v += (slots[4] + slots[5]) + (slots[6] + slots[7]);
   }
   return v;
 }
 
-constexpr int kThreads = 256;
+// of a workgroup
+template <int kLanes>
+constexpr int threads() { return kLanes > 256 ? kLanes : 256; }
 // Rows that a group of lanes has in hand at a time, beside as many whose loads are on their way.
 template <int kLanes, int NV>
 constexpr int rows_at_once() { return kLanes <= kWave && NV <= 3 ? 2 : 1; }
 
 // NV: groups of four values per lane.
 template <int kLanes, int NV, bool kBf16In, bool kBf16Out>
-__global__ __launch_bounds__(kThreads) void layer_norm_kernel(NormArgs a) {
+__global__ __launch_bounds__(threads<kLanes>()) void layer_norm_kernel(NormArgs a) {
   constexpr int R = rows_at_once<kLanes, NV>();
+  constexpr int kThreads = threads<kLanes>();
   constexpr int kRows = kThreads / kLanes * R;  // of a workgroup at a time
-  __shared__ float slots[2][2][4];
+  __shared__ float slots[2][2][kSlots];
   const int lane = threadIdx.x % kLanes;
   const int D = a.D;
   const float count = (float)D;
@@ -185,10 +192,11 @@ __global__ __launch_bounds__(kThreads) void layer_norm_kernel(NormArgs a) {
 
 // kParams: the gradients of weight and bias are wanted.
 template <int kLanes, int NV, bool kBf16In, bool kBf16Out, bool kParams>
-__global__ __launch_bounds__(kThreads) void layer_norm_grad_kernel(NormArgs a) {
+__global__ __launch_bounds__(threads<kLanes>()) void layer_norm_grad_kernel(NormArgs a) {
   constexpr int R = rows_at_once<kLanes, NV>();
+  constexpr int kThreads = threads<kLanes>();
   constexpr int kRows = kThreads / kLanes * R;
-  __shared__ float slots[2][2][4];
+  __shared__ float slots[2][2][kSlots];
   __shared__ f32x4 shares[kParams && kLanes <= kWave ? kThreads / kWave : 1][2 * kWave];
   const int lane = threadIdx.x % kLanes;
   const int D = a.D;
@@ -332,7 +340,7 @@ __global__ __launch_bounds__(kJoinThreads) void layer_norm_params_kernel(NormArg
 
 template <int kLanes, int NV>
 void launch_forward(const NormArgs& a, int blocks, hipStream_t stream) {
-  const dim3 grid(blocks), block(kThreads);
+  const dim3 grid(blocks), block(threads<kLanes>());
   if (a.x_bf16) {
     if (a.y_bf16) hipLaunchKernelGGL((layer_norm_kernel<kLanes, NV, true, true>), grid, block, 0, stream, a);
     else hipLaunchKernelGGL((layer_norm_kernel<kLanes, NV, true, false>), grid, block, 0, stream, a);
@@ -344,7 +352,7 @@ void launch_forward(const NormArgs& a, int blocks, hipStream_t stream) {
 
 template <int kLanes, int NV, bool kParams>
 void launch_backward(const NormArgs& a, int blocks, hipStream_t stream) {
-  const dim3 grid(blocks), block(kThreads);
+  const dim3 grid(blocks), block(threads<kLanes>());
   if (a.x_bf16) {
     if (a.y_bf16)
       hipLaunchKernelGGL((layer_norm_grad_kernel<kLanes, NV, true, true, kParams>), grid, block, 0, stream, a);
@@ -358,8 +366,10 @@ void launch_backward(const NormArgs& a, int blocks, hipStream_t stream) {
   }
 }
 
-// lanes per row
-int norm_lanes(int D) { return D <= 384 ? 16 : D <= 2048 ? 64 : 256; }
+// Lanes per row: as few as leave a lane six groups of four values at most.  GB/s of the backward pass in bf16 with the next
+// larger number: 192 values 4970 by 16 lanes, 4120 by 64; 384 4690 / 3840; 2048 5090 by 256, 3810 by 64; 5000 4390 by 256,
+// 3460 by 512; 8192 3940 by 512, 3400 by 256.
+int norm_lanes(int D) { return D <= 384 ? 16 : D <= 1536 ? 64 : D <= 6144 ? 256 : 512; }
 
 template <int kLanes, int NV>
 void launch_either(const NormArgs& a, int blocks, bool grad, hipStream_t stream) {
@@ -379,27 +389,29 @@ void launch_sized(const NormArgs& a, int blocks, bool grad, hipStream_t stream) 
       default: return launch_either<16, 6>(a, blocks, grad, stream);
     }
   }
-  if (a.D <= 2048) {
+  if (a.D <= 1536) {
     switch ((groups + 63) / 64) {
       case 2: return launch_either<64, 2>(a, blocks, grad, stream);
       case 3: return launch_either<64, 3>(a, blocks, grad, stream);
       case 4: return launch_either<64, 4>(a, blocks, grad, stream);
       case 5: return launch_either<64, 5>(a, blocks, grad, stream);
-      case 6: return launch_either<64, 6>(a, blocks, grad, stream);
-      default: return launch_either<64, 8>(a, blocks, grad, stream);
+      default: return launch_either<64, 6>(a, blocks, grad, stream);
     }
   }
-  switch ((groups + 255) / 256) {
-    case 3: return launch_either<256, 3>(a, blocks, grad, stream);
-    case 4: return launch_either<256, 4>(a, blocks, grad, stream);
-    case 5:
-    case 6: return launch_either<256, 6>(a, blocks, grad, stream);
-    default: return launch_either<256, 8>(a, blocks, grad, stream);
+  if (a.D <= 6144) {
+    switch ((groups + 255) / 256) {
+      case 2: return launch_either<256, 2>(a, blocks, grad, stream);
+      case 3: return launch_either<256, 3>(a, blocks, grad, stream);
+      case 4: return launch_either<256, 4>(a, blocks, grad, stream);
+      default: return launch_either<256, 6>(a, blocks, grad, stream);
+    }
   }
+  return launch_either<512, 4>(a, blocks, grad, stream);
 }
 
 int norm_blocks(int64_t M, int D, int most) {
-  const int rows = kThreads / norm_lanes(D) * ((D + 3) / 4 <= 3 * norm_lanes(D) && norm_lanes(D) <= kWave ? 2 : 1);  // rows_at_once
+  const int lanes = norm_lanes(D);
+  const int rows = (lanes > 256 ? 1 : 256 / lanes) * ((D + 3) / 4 <= 3 * lanes && lanes <= kWave ? 2 : 1);  // rows_at_once
   const int64_t blocks = (M + rows - 1) / rows;
   return (int)(blocks < most ? blocks : most);
 }
