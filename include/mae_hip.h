@@ -352,7 +352,8 @@ int mae_patch_embed(const mae_embed_desc* d, void* tokens, void* hip_stream);
  * order (two calls give the same bits).  `weight`, `bias` and the values of `pos` are not read.
  *
  * Limits: those of mae_patch_embed, out_dtype = MAE_BF16 (MAE_ERR_DTYPE otherwise), and with `pos`
- * L <= 8192.  grad_tokens and grad_weight are 16-byte aligned.
+ * L <= 8192 (the work of grad_pos grows with L).  grad_tokens and grad_weight are 16-byte aligned.  Outputs do
+ * not overlap inputs.  Which of the three are asked for does not change their bits.
  *   grad_weight [E, D] float, grad_bias [E] float, grad_pos [L, E] float    each nullable, not all;
  *                                           grad_pos only with `pos` in the descriptor
  *   workspace   mae_patch_embed_grad_workspace_bytes(d) bytes, 256-byte aligned (0: invalid descriptor) */
@@ -453,7 +454,7 @@ size_t mae_layer_norm_workspace_bytes(const mae_norm_desc* d);
  * grad_bias is summed before that rounding.  A class whose bias is -infinity or the lowest float has probability 0.
  *
  * Limits: 1 <= M <= 2^24, 8 <= D <= 8192 with D % 8 == 0, 1 <= V <= 2^20, M * V <= 2^38.
- * tokens, weight, grad_tokens and grad_weight are 16-byte aligned.
+ * tokens, weight, grad_tokens and grad_weight are 16-byte aligned.  Outputs do not overlap inputs.
  * ---------------------------------------------------------------------------------------------- */
 typedef struct {
   int64_t M;

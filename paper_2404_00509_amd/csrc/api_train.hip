@@ -161,7 +161,7 @@ int mae_dropout(const mae_dropout_desc* d, void* y, void* hip_stream) {
 
 size_t mae_class_loss_workspace_bytes(const mae_class_desc* d, int32_t with_grad) {
   if (validate_class(d) != MAE_OK) return 0;
-  return mae::class_plan(d->M, d->D, d->V, with_grad != 0).bytes;
+  return mae::class_plan(d->M, d->D, d->V, d->smoothing > 0.0f, with_grad != 0).bytes;
 }
 
 int mae_class_loss(const mae_class_desc* d, float* loss, float* row_loss, void* grad_tokens, void* grad_weight,
@@ -174,7 +174,7 @@ int mae_class_loss(const mae_class_desc* d, float* loss, float* row_loss, void* 
       !aligned(grad_bias, 4))
     return MAE_ERR_RANGE;
   const bool grad = grad_tokens || grad_weight || grad_bias;
-  const mae::ClassPlan p = mae::class_plan(d->M, d->D, d->V, grad);
+  const mae::ClassPlan p = mae::class_plan(d->M, d->D, d->V, d->smoothing > 0.0f, grad);
   if (!has_workspace(workspace, workspace_bytes, p.bytes)) return MAE_ERR_WORKSPACE;
   rc = have_device();
   if (rc != MAE_OK) return rc;

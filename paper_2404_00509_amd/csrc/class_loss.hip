@@ -28,9 +28,15 @@
 // Types.  Logits: products of the bf16 operands, fp32 sums.  Maxima, exponentials and their sums: fp32; sums over rows of
 // the loss: double precision.  g, an operand of two products, is fp16 and not bf16: |g| <= 1, so that as 2^15 g it
 // loses at most 2^-11 of a value down to 2^-29, an eighth of what bf16 would, and less than the bf16 outputs
-// do by their own rounding (with bf16 a gradient of few rows and classes was up to 2.5 times as far from the exact one as
-// a result that is rounded once).  The other operand has to be fp16 too: scaled by the power of two that puts its largest value just
-// under 2^15, a bf16 number down to 2^-32 of that is exact.
+// do by their own rounding (with bf16 gradients were up to 1.5 times as far from the exact ones as results that are
+// rounded once, now within 1 %).  The other operand has to be fp16 too: scaled by the power of two that puts its
+// largest value just under 2^15, a bf16 number down to 2^-32 of that is exact.
+//
+// 16,384 x 1024 over 32,003 classes, a tenth of the rows left out, 3.87 TFLOP with the logits made twice: 3.6 to 3.7 ms.
+// pack 26 us, stats 940 (1.03 PFLOP/s), rows 48, and twice grad 510 and products 870 (1.13 PFLOP/s).  What bounds it is
+// the main loop (matmul.hpp), and beside it in stats and grad the exponentials: a tile of 256 x 256 with 16 slices
+// takes 33 us, 26 of them in the loop.  Small calls are bound by their launches: 64 x 192 over 1000 classes 28 us
+// for six, 4.5 us each.
 #include "mae_device.hpp"
 #include "mae_kernels.hpp"
 #include "matmul.hpp"
@@ -85,7 +91,7 @@ __device__ inline int half_exponent(int32_t peak) {
   const int e = (peak >> 7) - 127;  // 2^e <= the largest value < 2^(e + 1)
   return min(14 - e, 126);
 }
-// largest of the peaks [from, to), by all lanes of a wavefront
+// Largest of the peaks [from, to), by all lanes of a wavefront
 __device__ inline int32_t peak_among(const int32_t* peaks, int from, int to) {
   int32_t p = 0;
   for (int i = from + (int)(threadIdx.x % kWave); i < to; i += kWave) p = max(p, peaks[i]);
@@ -266,84 +272,84 @@ __global__ __launch_bounds__(64 * WGM * WGN) void class_stats_kernel(ClassArgs a
   typename T::Place next = T::place(a, blockIdx.x, tiles, count, 0, a.V);
   T::template fill<0, 4>(next.source, lds);
   for (uint32_t id = blockIdx.x; id < tiles; id += gridDim.x) {
-  const typename T::Place at = next;
-  f32x16 acc[TM][TN];
-  T::template run<4>(at.source, lds, acc);
-  const int v0 = at.c0, rows_v = at.rows_v, rows_n = at.rows_n;
-  const int64_t n0 = at.n0;
-  const int first = v0 + wm * 32 * TM;
-  __syncthreads();  // every wavefront is done with the ring
-  if (id + gridDim.x < tiles) {
-    next = T::place(a, id + gridDim.x, tiles, count, 0, a.V);
-    T::template fill<0, 4>(next.source, lds);
-  }
-  add_bias<TM, TN>(a.bias, first, a.V, lane, acc);
-  const int half = 4 * (lane >> 5);
-  const int classes = a.V - first - half;  // class 32 i + 8 (e / 4) + e % 4 of this lane exists if below
+    const typename T::Place at = next;
+    f32x16 acc[TM][TN];
+    T::template run<4>(at.source, lds, acc);
+    const int v0 = at.c0, rows_v = at.rows_v, rows_n = at.rows_n;
+    const int64_t n0 = at.n0;
+    const int first = v0 + wm * 32 * TM;
+    __syncthreads();  // every wavefront is done with the ring
+    if (id + gridDim.x < tiles) {
+      next = T::place(a, id + gridDim.x, tiles, count, 0, a.V);
+      T::template fill<0, 4>(next.source, lds);
+    }
+    add_bias<TM, TN>(a.bias, first, a.V, lane, acc);
+    const int half = 4 * (lane >> 5);
+    const int classes = a.V - first - half;  // class 32 i + 8 (e / 4) + e % 4 of this lane exists if below
 #pragma unroll
-  for (int j = 0; j < TN; ++j) {
-    const int r = wn * 32 * TN + j * 32 + (lane & 31);
-    const int y = r < rows_n ? a.label_of[n0 + r] - first - half : -1;
-    float sl = 0.f;
-    if (a.logit_sums) {
+    for (int j = 0; j < TN; ++j) {
+      const int r = wn * 32 * TN + j * 32 + (lane & 31);
+      const int y = r < rows_n ? a.label_of[n0 + r] - first - half : -1;
+      float sl = 0.f;
+      if (a.logit_sums) {
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) sl += 32 * i + 8 * (e >> 2) + (e & 3) < classes ? acc[i][j][e] : 0.f;
+      }
+      if (rows_v < T::BM) {
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) acc[i][j][e] = 32 * i + 8 * (e >> 2) + (e & 3) < classes ? acc[i][j][e] : kNegInf;
+      }
+      // the label's logit: few rows have theirs among a wavefront's classes
+      const bool mine = y >= 0 && y < 32 * TM && (y & 4) == 0;
+      if (__any(mine)) {
+        float own = 0.f;
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) own = 32 * i + 8 * (e >> 2) + (e & 3) == y ? acc[i][j][e] : own;
+        if (mine) a.label_logit[n0 + r] = own;
+      }
+      float m = acc[0][j][0];
 #pragma unroll
       for (int i = 0; i < TM; ++i)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) sl += 32 * i + 8 * (e >> 2) + (e & 3) < classes ? acc[i][j][e] : 0.f;
-    }
-    if (rows_v < T::BM) {
+        for (int e = 0; e < 16; ++e) m = fmaxf(m, acc[i][j][e]);
+      m = fmaxf(m, __shfl_xor(m, 32, kWave));
+      const float from = m == kNegInf ? 0.f : m;  // (a tile of -inf only adds nothing; a NaN reaches the sum)
+      float s = 0.f;
 #pragma unroll
       for (int i = 0; i < TM; ++i)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) acc[i][j][e] = 32 * i + 8 * (e >> 2) + (e & 3) < classes ? acc[i][j][e] : kNegInf;
+        for (int e = 0; e < 16; ++e) s += exp_neg(acc[i][j][e] - from);
+      s += __shfl_xor(s, 32, kWave);
+      sl += __shfl_xor(sl, 32, kWave);
+      if (lane < 32) {
+        float* p = part + (wm * T::BN + r) * 3;
+        p[0] = m;
+        p[1] = s;
+        p[2] = sl;
+      }
     }
-    // the label's logit: few rows have theirs among a wavefront's classes
-    const bool mine = y >= 0 && y < 32 * TM && (y & 4) == 0;
-    if (__any(mine)) {
-      float own = 0.f;
+    __syncthreads();
+    for (int r = tid; r < rows_n; r += T::kThreads) {
+      float m = kNegInf, s = 0.f, sl = 0.f;
 #pragma unroll
-      for (int i = 0; i < TM; ++i)
+      for (int w = 0; w < WGM; ++w) m = fmaxf(m, part[(w * T::BN + r) * 3]);
 #pragma unroll
-        for (int e = 0; e < 16; ++e) own = 32 * i + 8 * (e >> 2) + (e & 3) == y ? acc[i][j][e] : own;
-      if (mine) a.label_logit[n0 + r] = own;
+      for (int w = 0; w < WGM; ++w) {
+        const float* p = part + (w * T::BN + r) * 3;
+        s += p[0] == kNegInf ? p[1] : p[1] * exp_neg(p[0] - m);
+        sl += p[2];
+      }
+      const int64_t to = (n0 + r) * (int64_t)a.stat_tiles + at.tv;
+      reinterpret_cast<f32x2*>(a.stats)[to] = f32x2{m, s};
+      if (a.logit_sums) a.logit_sums[to] = sl;
     }
-    float m = acc[0][j][0];
-#pragma unroll
-    for (int i = 0; i < TM; ++i)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) m = fmaxf(m, acc[i][j][e]);
-    m = fmaxf(m, __shfl_xor(m, 32, kWave));
-    const float from = m == kNegInf ? 0.f : m;  // (a tile of -inf only adds nothing; a NaN reaches the sum)
-    float s = 0.f;
-#pragma unroll
-    for (int i = 0; i < TM; ++i)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) s += exp_neg(acc[i][j][e] - from);
-    s += __shfl_xor(s, 32, kWave);
-    sl += __shfl_xor(sl, 32, kWave);
-    if (lane < 32) {
-      float* p = part + (wm * T::BN + r) * 3;
-      p[0] = m;
-      p[1] = s;
-      p[2] = sl;
-    }
-  }
-  __syncthreads();
-  for (int r = tid; r < rows_n; r += T::kThreads) {
-    float m = kNegInf, s = 0.f, sl = 0.f;
-#pragma unroll
-    for (int w = 0; w < WGM; ++w) m = fmaxf(m, part[(w * T::BN + r) * 3]);
-#pragma unroll
-    for (int w = 0; w < WGM; ++w) {
-      const float* p = part + (w * T::BN + r) * 3;
-      s += p[0] == kNegInf ? p[1] : p[1] * exp_neg(p[0] - m);
-      sl += p[2];
-    }
-    const int64_t to = (n0 + r) * (int64_t)a.stat_tiles + at.tv;
-    reinterpret_cast<f32x2*>(a.stats)[to] = f32x2{m, s};
-    if (a.logit_sums) a.logit_sums[to] = sl;
-  }
-  __syncthreads();
+    __syncthreads();
   }
 }
 
@@ -512,112 +518,112 @@ __global__ __launch_bounds__(64 * WGM * WGN) void class_grad_kernel(ClassArgs a)
   typename T::Place next = T::place(a, blockIdx.x, tiles, count, a.piece_first, a.piece_classes);
   T::template fill<0, 2>(next.source, lds);
   for (uint32_t id = blockIdx.x; id < tiles; id += gridDim.x) {
-  const typename T::Place at = next;
-  f32x16 acc[TM][TN];
-  T::template run<2>(at.source, lds, acc);
-  const int c0 = at.c0, rows_v = at.rows_v, rows_n = at.rows_n;
-  const int64_t n0 = at.n0;
-  const int first = a.piece_first + c0 + wm * 32 * TM;
-  __syncthreads();  // every wavefront is done with the ring
-  if (id + gridDim.x < tiles) {
-    next = T::place(a, id + gridDim.x, tiles, count, a.piece_first, a.piece_classes);
-    T::template fill<0, 2>(next.source, lds);
-  }
-  add_bias<TM, TN>(a.bias, first, a.V, lane, acc);
+    const typename T::Place at = next;
+    f32x16 acc[TM][TN];
+    T::template run<2>(at.source, lds, acc);
+    const int c0 = at.c0, rows_v = at.rows_v, rows_n = at.rows_n;
+    const int64_t n0 = at.n0;
+    const int first = a.piece_first + c0 + wm * 32 * TM;
+    __syncthreads();  // every wavefront is done with the ring
+    if (id + gridDim.x < tiles) {
+      next = T::place(a, id + gridDim.x, tiles, count, a.piece_first, a.piece_classes);
+      T::template fill<0, 2>(next.source, lds);
+    }
+    add_bias<TM, TN>(a.bias, first, a.V, lane, acc);
 
-  const float uniform = a.smoothing / (float)a.V * kGScale, label = (1.0f - a.smoothing) * kGScale;
-  const int half = 4 * (lane >> 5);
-  const int classes = a.piece_first + a.piece_classes - first - half;  // of the piece, from this lane's first one on
+    const float uniform = a.smoothing / (float)a.V * kGScale, label = (1.0f - a.smoothing) * kGScale;
+    const int half = 4 * (lane >> 5);
+    const int classes = a.piece_first + a.piece_classes - first - half;  // of the piece, from this lane's first one on
 #pragma unroll
-  for (int j = 0; j < TN; ++j) {
-    const int r = wn * 32 * TN + j * 32 + (lane & 31);
-    const bool live = r < rows_n;  // (a row that does not exist gets zeros)
-    const float m = live ? a.row_max[n0 + r] : __builtin_inff(), inv = live ? a.row_inv[n0 + r] * kGScale : 0.f;
-    const float off = live ? uniform : 0.f;
-    const int y = live ? a.label_of[n0 + r] - first - half : -1;
-#pragma unroll
-    for (int i = 0; i < TM; ++i)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) acc[i][j][e] = exp_neg(acc[i][j][e] - m) * inv - off;
-    if (__any(y >= 0 && y < 32 * TM)) {  // few rows have their label among a wavefront's classes
+    for (int j = 0; j < TN; ++j) {
+      const int r = wn * 32 * TN + j * 32 + (lane & 31);
+      const bool live = r < rows_n;  // (a row that does not exist gets zeros)
+      const float m = live ? a.row_max[n0 + r] : __builtin_inff(), inv = live ? a.row_inv[n0 + r] * kGScale : 0.f;
+      const float off = live ? uniform : 0.f;
+      const int y = live ? a.label_of[n0 + r] - first - half : -1;
 #pragma unroll
       for (int i = 0; i < TM; ++i)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) acc[i][j][e] -= 32 * i + 8 * (e >> 2) + (e & 3) == y ? label : 0.f;
-    }
-    if (rows_v < T::BM) {
+        for (int e = 0; e < 16; ++e) acc[i][j][e] = exp_neg(acc[i][j][e] - m) * inv - off;
+      if (__any(y >= 0 && y < 32 * TM)) {  // few rows have their label among a wavefront's classes
 #pragma unroll
-      for (int i = 0; i < TM; ++i)
+        for (int i = 0; i < TM; ++i)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) acc[i][j][e] = 32 * i + 8 * (e >> 2) + (e & 3) < classes ? acc[i][j][e] : 0.f;
-    }
-#pragma unroll
-    for (int i = 0; i < TM; ++i)
-#pragma unroll
-      for (int q = 0; q < 4; ++q)
-        *reinterpret_cast<u32x2*>(strip + (lane & 31) * kPitch + 32 * i + 8 * q + half) =
-            u32x2{half_pair(acc[i][j][4 * q], acc[i][j][4 * q + 1]), half_pair(acc[i][j][4 * q + 2], acc[i][j][4 * q + 3])};
-    __builtin_amdgcn_wave_barrier();
-    // rows of the strip to memory, 16 bytes per lane
-    constexpr int kLanesPerRow = 4 * TM;
-    constexpr int kRowsPerRep = kWave / kLanesPerRow;
-#pragma unroll
-    for (int rep = 0; rep < 32 / kRowsPerRep; ++rep) {
-      const int sr = rep * kRowsPerRep + lane / kLanesPerRow;
-      const int col = (lane % kLanesPerRow) * 8;
-      const u32x4 v = *reinterpret_cast<const u32x4*>(strip + sr * kPitch + col);
-      const int row = wn * 32 * TN + j * 32 + sr;
-      const int c = c0 + wm * 32 * TM + col;
-      if (row < rows_n && c < a.piece_ld)
-        *reinterpret_cast<u32x4*>(a.g + (n0 + row) * (int64_t)a.piece_ld + c) = v;
-    }
-    __builtin_amdgcn_wave_barrier();
-  }
-  if (a.column_sums) {
-  // sums over the tile's rows: over j in registers, over 32 lanes by halving, over wavefronts through LDS
-  float v[16 * TM];
-#pragma unroll
-  for (int i = 0; i < TM; ++i)
-#pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      float s = acc[i][0][e];
-#pragma unroll
-      for (int j = 1; j < TN; ++j) s += acc[i][j][e];
-      v[16 * i + e] = s;
-    }
-  constexpr int N = 16 * TM;
-  halve<N, 16>(v, lane);
-  halve<(N > 1 ? N / 2 : 1), 8>(v, lane);
-  halve<(N > 2 ? N / 4 : 1), 4>(v, lane);
-  halve<(N > 4 ? N / 8 : 1), 2>(v, lane);
-  halve<(N > 8 ? N / 16 : 1), 1>(v, lane);
-  // the index of what is left: the lane's bits from the top down, then k
-  constexpr int kLeft = N >= 32 ? N / 32 : 1;
-  int base = 0;
-  {
-    int n = N;
-#pragma unroll
-    for (int mask = 16; mask > 0; mask >>= 1)
-      if (n > 1) {
-        n >>= 1;
-        if (lane & mask) base += n;
+          for (int e = 0; e < 16; ++e) acc[i][j][e] -= 32 * i + 8 * (e >> 2) + (e & 3) == y ? label : 0.f;
       }
-  }
+      if (rows_v < T::BM) {
 #pragma unroll
-  for (int k = 0; k < kLeft; ++k) {
-    const int at = base + k, i = at >> 4, e = at & 15;
-    const int c = wm * 32 * TM + 32 * i + 8 * (e >> 2) + half + (e & 3);
-    columns[wn * T::BM + c] = v[k];  // (lanes that hold the same sum write the same value)
-  }
-  __syncthreads();
-  for (int c = tid; c < rows_v; c += T::kThreads) {
-    float s = columns[c];
+        for (int i = 0; i < TM; ++i)
 #pragma unroll
-    for (int w = 1; w < WGN; ++w) s += columns[w * T::BM + c];
-    a.column_sums[(int64_t)at.tn * a.piece_classes + c0 + c] = s;
-  }
-  }
-  __syncthreads();
+          for (int e = 0; e < 16; ++e) acc[i][j][e] = 32 * i + 8 * (e >> 2) + (e & 3) < classes ? acc[i][j][e] : 0.f;
+      }
+#pragma unroll
+      for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          *reinterpret_cast<u32x2*>(strip + (lane & 31) * kPitch + 32 * i + 8 * q + half) =
+              u32x2{half_pair(acc[i][j][4 * q], acc[i][j][4 * q + 1]), half_pair(acc[i][j][4 * q + 2], acc[i][j][4 * q + 3])};
+      __builtin_amdgcn_wave_barrier();
+      // rows of the strip to memory, 16 bytes per lane
+      constexpr int kLanesPerRow = 4 * TM;
+      constexpr int kRowsPerRep = kWave / kLanesPerRow;
+#pragma unroll
+      for (int rep = 0; rep < 32 / kRowsPerRep; ++rep) {
+        const int sr = rep * kRowsPerRep + lane / kLanesPerRow;
+        const int col = (lane % kLanesPerRow) * 8;
+        const u32x4 v = *reinterpret_cast<const u32x4*>(strip + sr * kPitch + col);
+        const int row = wn * 32 * TN + j * 32 + sr;
+        const int c = c0 + wm * 32 * TM + col;
+        if (row < rows_n && c < a.piece_ld)
+          *reinterpret_cast<u32x4*>(a.g + (n0 + row) * (int64_t)a.piece_ld + c) = v;
+      }
+      __builtin_amdgcn_wave_barrier();
+    }
+    if (a.column_sums) {
+      // sums over the tile's rows: over j in registers, over 32 lanes by halving, over wavefronts through LDS
+      float v[16 * TM];
+#pragma unroll
+      for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          float s = acc[i][0][e];
+#pragma unroll
+          for (int j = 1; j < TN; ++j) s += acc[i][j][e];
+          v[16 * i + e] = s;
+        }
+      constexpr int N = 16 * TM;
+      halve<N, 16>(v, lane);
+      halve<(N > 1 ? N / 2 : 1), 8>(v, lane);
+      halve<(N > 2 ? N / 4 : 1), 4>(v, lane);
+      halve<(N > 4 ? N / 8 : 1), 2>(v, lane);
+      halve<(N > 8 ? N / 16 : 1), 1>(v, lane);
+      // the index of what is left: the lane's bits from the top down, then k
+      constexpr int kLeft = N >= 32 ? N / 32 : 1;
+      int base = 0;
+      {
+        int n = N;
+#pragma unroll
+        for (int mask = 16; mask > 0; mask >>= 1)
+          if (n > 1) {
+            n >>= 1;
+            if (lane & mask) base += n;
+          }
+      }
+#pragma unroll
+      for (int k = 0; k < kLeft; ++k) {
+        const int at = base + k, i = at >> 4, e = at & 15;
+        const int c = wm * 32 * TM + 32 * i + 8 * (e >> 2) + half + (e & 3);
+        columns[wn * T::BM + c] = v[k];  // (lanes that hold the same sum write the same value)
+      }
+      __syncthreads();
+      for (int c = tid; c < rows_v; c += T::kThreads) {
+        float s = columns[c];
+#pragma unroll
+        for (int w = 1; w < WGN; ++w) s += columns[w * T::BM + c];
+        a.column_sums[(int64_t)at.tn * a.piece_classes + c0 + c] = s;
+      }
+    }
+    __syncthreads();
   }
 }
 
@@ -815,7 +821,7 @@ static int products_side(int64_t M, int D, int V) {
   return M <= 256 || tiles(256) < 256 ? 128 : 256;
 }
 
-ClassPlan class_plan(int64_t M, int D, int V, bool grad) {
+ClassPlan class_plan(int64_t M, int D, int V, bool smooth, bool grad) {
   ClassPlan p{};
   p.few = !grad && M <= kFewRows;
   p.side = logits_side(M, V);
@@ -830,7 +836,7 @@ ClassPlan class_plan(int64_t M, int D, int V, bool grad) {
   };
   const size_t m = (size_t)M;
   p.stats = take(m * p.stat_tiles * 8);
-  p.logit_sums = take(m * p.stat_tiles * 4);
+  p.logit_sums = take(smooth ? m * p.stat_tiles * 4 : 0);
   p.label_logit = take(m * 4);
   if (!p.few) {
     p.count = take(sizeof(int32_t));

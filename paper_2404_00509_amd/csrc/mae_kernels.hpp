@@ -291,7 +291,7 @@ struct ClassPlan {
   size_t peaks, row_max, row_inv, half_tokens, half_weight, g, column_sums, tokens_acc, weight_acc;
   size_t bytes;
 };
-ClassPlan class_plan(int64_t M, int D, int V, bool grad);
+ClassPlan class_plan(int64_t M, int D, int V, bool smooth, bool grad);
 struct ClassArgs {
   int64_t M;
   int32_t D, V;

@@ -20,7 +20,16 @@
 // the swizzle is applied on the global side.
 //
 // Fragment reads are inline assembly, so that the compiler does not make each of them wait for every
-// direct load in flight; the code waits on lgkmcnt itself before it uses what was read.
+// direct load in flight; the code waits on lgkmcnt itself before it uses what was read, in straight lines, and
+// a test goes through the assembly for registers that are touched in between (spilled or moved, as under
+// more register pressure they are).
+//
+// What bounds it.  A slice of a 256 x 256 tile takes 1.62 us on the 256 compute units together (1.3 PFLOP/s): its
+// multiplies alone take 1.00 us at 2.28 GHz, with the reads beside them 1.31 us at 1.8 GHz, with the loads too 1.62 us at
+// 1.45 to 1.75 GHz, where 2048 of 2350 to 2800 cycles multiply: the card's clock falls with the power of the three together.
+// Tried: four wavefronts of 128 x 128 (a third less to read, but a wavefront alone on its SIMD waits for its own
+// loads: 1.7 us), loads at other multiplies for each wavefront (branches: 1.85 us), reads behind the first one, two or four of
+// eight multiplies instead of six (the same), rows on an odd number of lines (the same).
 #pragma once
 
 #include "mae_device.hpp"
@@ -218,7 +227,7 @@ struct Tile {
     const int lane = threadIdx.x % kWave;
     const int wave = uniform((int)threadIdx.x / kWave);
     const int wm = wave / WGN, wn = wave % WGN;
-    const int nk = src.nk, tail = src.tail;
+    const int nk = src.nk;
 #pragma unroll
     for (int i = 0; i < TM; ++i)
 #pragma unroll
@@ -392,23 +401,17 @@ struct Tile {
       pa = na;
       pb = nb;
     }
-    const int left = tail ? (tail + 15) / 16 : 4;  // sub-steps of the last slice that hold values
-    if (left > 1) read_frags(pa, pb, Tag<1>{}, 1);
+    // The last slice (behind the end of k it holds zeros).
+    read_frags(pa, pb, Tag<1>{}, 1);
     multiply(0);
-    if (left > 1) {
-      arrive(1);
-      if (left > 2) read_frags(pa, pb, Tag<2>{}, 0);
-      multiply(1);
-    }
-    if (left > 2) {
-      arrive(0);
-      if (left > 3) read_frags(pa, pb, Tag<3>{}, 1);
-      multiply(0);
-    }
-    if (left > 3) {
-      arrive(1);
-      multiply(1);
-    }
+    arrive(1);
+    read_frags(pa, pb, Tag<2>{}, 0);
+    multiply(1);
+    arrive(0);
+    read_frags(pa, pb, Tag<3>{}, 1);
+    multiply(0);
+    arrive(1);
+    multiply(1);
   }
 
  private:

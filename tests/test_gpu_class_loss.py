@@ -5,7 +5,7 @@ import pytest
 import torch
 
 import paper_2404_00509_amd as mae
-from train_reference import check, class_loss
+from train_reference import U16, check, class_loss
 
 pytestmark = pytest.mark.gpu
 
@@ -155,6 +155,57 @@ def test_sizes_of_the_operands(of_tokens, of_weight):
     big[::2] = 3e38
     out, clean = _run(big, gone, w, b, 0.1), _run(x, gone, w, b, 0.1)
     assert all(torch.equal(out[k], clean[k]) for k in out)
+
+
+@pytest.mark.parametrize("M", [1, 2, 7, 33, 63, 64, 65, 130])
+@pytest.mark.parametrize("D,V", [(8, 3), (200, 1003), (1024, 20011)])
+def test_the_loss_alone_of_few_rows(M, D, V):
+    for bias, smoothing, left_out in ((True, 0.1, 0.4), (False, 0.0, 0.0)):
+        x, y, w, b = _inputs(14, M, D, V, bias, left_out)
+        ref, bound = class_loss(x, y, w, b, smoothing)
+        x[(y < 0)] = float("nan")
+        out = _run(x, y, w, b, smoothing, want=())
+        for k, v in out.items():
+            check(v, ref[k], bound[k], f"M{M} D{D} V{V} {k}")
+        gone = _run(x, torch.full_like(y, V), w, b, smoothing, want=())
+        assert not gone["loss"].any() and not gone["row_loss"].any()
+
+
+def test_the_largest_width_and_pointers_on_their_values_boundaries():
+    x, y, w, b = _inputs(15, 70, 8192, 330, True, 0.1)
+    out = _check(x, y, w, b, 0.1, what="D8192")
+    moved = [torch.cat([t.new_zeros(1), t])[1:] for t in (y, b)]
+    assert all(t.data_ptr() % 8 for t in moved)
+    again = _run(x, moved[0], w, moved[1], 0.1)
+    assert all(torch.equal(out[k], again[k]) for k in out)
+
+
+def test_offsets_past_32_bits():
+    # more than 2^31 token values and 2^32 bytes; few classes, so that everything else stays small
+    M, D, V = 600_000, 4096, 24
+    g = torch.Generator(device="cuda").manual_seed(1)
+    base = torch.randn(3001, D, generator=g, device="cuda").to(BF16)  # rows repeat with an odd period
+    x = base.repeat(M // 3001 + 1, 1)[:M].contiguous()
+    w = (torch.randn(V, D, generator=g, device="cuda") / 64).to(BF16)
+    y = torch.randint(-3, V, (M,), generator=g, device="cuda", dtype=torch.int32)
+    out = _run(x, y, w, None)
+    n = int((y >= 0).sum())
+    for rows in (slice(0, 900), slice(300_000, 300_900), slice(M - 900, M)):
+        ref, bound = class_loss(x[rows], y[rows], w, None, 0.0)
+        share = int((y[rows] >= 0).sum()) / n  # the reference divides by its own number of rows
+        check(out["row_loss"][rows], ref["row_loss"], bound["row_loss"], "row_loss")
+        check(out["grad_tokens"][rows], ref["grad_tokens"] * share, bound["grad_tokens"] * share, "grad_tokens")
+    # the weight's gradient: sums over equal rows first
+    l = base.double() @ w.double().T.contiguous()
+    p = torch.softmax(l, 1)
+    at = torch.arange(M, device="cuda") % 3001
+    counts = torch.zeros(3001, V + 1, dtype=torch.float64, device="cuda")
+    flat = at * (V + 1) + torch.where(y >= 0, y.long(), torch.full_like(at, V))
+    counts.view(-1).index_add_(0, flat, torch.ones(M, dtype=torch.float64, device="cuda"))
+    gsum = p * counts[:, :V].sum(1, keepdim=True) - counts[:, :V]
+    want = gsum.T.contiguous() @ base.double() / n
+    off = (out["grad_weight"].double() - want).norm() / want.norm()
+    assert float(off) < 2.5 * U16  # one rounding of the result, an eighth of it for g, fp32 sums of 600,000 terms
 
 
 def test_each_output_by_itself():

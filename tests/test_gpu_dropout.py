@@ -143,6 +143,16 @@ def test_many_values():
         _check(x[a:b], None, dict(rows_per_draw=0, row_base=a, **key), part, f"rows {a}")
 
 
+@pytest.mark.parametrize("rows_per_draw", [0, 3])
+def test_offsets_past_32_bits(rows_per_draw):
+    M, D = 1_060_003, 2053  # more than 2^31 values and 2^32 bytes
+    x = torch.ones(M, D, dtype=BF16, device="cuda")
+    key = dict(p=0.1, rows_per_draw=rows_per_draw, seed=3, batch_index=1, layer=2)
+    y = _run(x, None, **key)
+    for a, b in ((0, 99), (1_046_000, 1_046_100), (M - 99, M)):
+        _check(x[a:b], None, dict(row_base=a, **key), y[a:b], f"rows {a}")
+
+
 def test_side_stream_and_replays_of_a_graph():
     x, residual = _inputs(8, 500, 768, BF16)
     key = dict(p=0.1, seed=21, batch_index=22, layer=23)

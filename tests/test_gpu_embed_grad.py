@@ -183,6 +183,21 @@ def test_side_stream_and_replays_of_a_graph():
         visible.mul_(1.0)
 
 
+def test_offsets_past_32_bits():
+    M, D, E, L = 2_200_001, 12, 1024, 30  # more than 2^31 gradient values and 2^32 bytes
+    base_v, base_g, base_ids = _whole(9, 2003, D, E, L, most=2)
+    visible, g = (t.repeat(M // 2003 + 1, 1)[:M].contiguous() for t in (base_v, base_g))
+    ids = base_ids.repeat(M // 2003 + 1)[:M].contiguous()
+    times = torch.full((2003, 1), float(M // 2003), dtype=torch.float64, device="cuda")
+    times[:M % 2003] += 1
+    weighted = base_g.double() * times
+    pos = torch.zeros(L, E, dtype=torch.float64, device="cuda").index_add_(0, base_ids.long(), weighted)
+    want = weighted.T.contiguous() @ base_v.double(), weighted.sum(0), pos
+    for got, ref, name in zip(_run(visible, g, ids, L), want, ("weight", "bias", "pos")):
+        assert float(ref.abs().max()) < 2 ** 24
+        assert torch.equal(got.double(), ref), name
+
+
 def test_after_the_input_pipeline():
     wl = synth.WORKLOADS["c1"]
     B, E = 16, 192

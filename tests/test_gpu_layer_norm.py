@@ -161,6 +161,29 @@ def test_in_place_and_nothing_behind_the_last_row(D):
         assert torch.equal(xx if over == "x" else gg, gx), over
 
 
+def test_offsets_past_32_bits():
+    M, D = 1_060_003, 2053  # more than 2^31 values and 2^32 bytes
+    base = _inputs(11, 1009, D, BF16, BF16)
+    x, gy = (t.repeat(M // 1009 + 1, 1)[:M].contiguous() for t in base[:2])
+    w, b = base[2:]
+    desc, y, mean, rstd = _forward(x, w, b, 1e-6, BF16)
+    gx, gw, gb = _backward(desc, x, gy, mean, rstd)
+    _, y1, mean1, rstd1 = _forward(*base[:1], w, b, 1e-6, BF16)
+    gx1 = _backward(mae.make_norm_desc(base[0], w, b), base[0], base[1], mean1, rstd1)[0]
+    for at in (0, 1009 * 500, 1009 * 1049):
+        assert torch.equal(y[at:at + 1009], y1) and torch.equal(gx[at:at + 1009], gx1)
+        assert torch.equal(mean[at:at + 1009], mean1) and torch.equal(rstd[at:at + 1009], rstd1)
+    tail = M % 1009
+    assert torch.equal(y[M - tail:], y1[:tail]) and torch.equal(gx[M - tail:], gx1[:tail])
+    h = (base[0].double() - mean1.double()[:, None]) * rstd1.double()[:, None]
+    times = torch.full((1009, 1), float(M // 1009), dtype=torch.float64, device="cuda")
+    times[:tail] += 1
+    n = (_rows_in_turn(M, D) + 12) * U32
+    g = base[1].double() * times
+    check(gw, (g * h).sum(0), (n + U32) * (g * h).abs().sum(0), "grad_weight")
+    check(gb, g.sum(0), (n + U32) * g.abs().sum(0), "grad_bias")
+
+
 def test_gradient_against_differences():
     M, D, h = 24, 96, 2.0 ** -6
     x, c, w, b = _inputs(9, M, D, F32, F32)
