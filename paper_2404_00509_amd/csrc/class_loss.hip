@@ -177,21 +177,25 @@ __global__ __launch_bounds__(kPackThreads) void class_pack_kernel(ClassArgs a) {
     if (r < end && !in && a.row_loss) a.row_loss[r] = 0.f;
     map[tid] = in ? slot : -1;
     __syncthreads();
-    // the tokens, a wavefront per row, 16 bytes per lane
-    const int rows = (int)min((int64_t)kPackThreads, end - base);
-    for (int i = wave; i < rows; i += kPackThreads / kWave) {
-      const int32_t to = map[i];
-      if (to >= 0) {
-        const u32x4* src = reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(a.tokens) + (base + i) * a.D);
-        u32x4* dst = reinterpret_cast<u32x4*>(a.packed + (int64_t)to * a.D);
-        for (int c = lane; c < a.D / 8; c += kWave) {
-          const u32x4 v = src[c];
-          if (a.peaks) peak = peak_of(peak, v);
-          dst[c] = v;
+    // the tokens, 16 bytes per lane, several loads in flight
+    const int per_row = a.D / 8, chunks = (int)min((int64_t)kPackThreads, end - base) * per_row;
+    const u32x4* src = reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(a.tokens) + base * a.D);
+    constexpr int kBatch = 8;
+    for (int i0 = tid; i0 < chunks; i0 += kBatch * kPackThreads) {
+      u32x4 v[kBatch];
+#pragma unroll
+      for (int k = 0; k < kBatch; ++k) v[k] = src[min(i0 + k * kPackThreads, chunks - 1)];
+#pragma unroll
+      for (int k = 0; k < kBatch; ++k) {
+        const int i = i0 + k * kPackThreads;
+        if (i >= chunks) break;
+        const int row = i / per_row, c = i - row * per_row, to = map[row];
+        if (to >= 0) {
+          if (a.peaks) peak = peak_of(peak, v[k]);
+          reinterpret_cast<u32x4*>(a.packed + (int64_t)to * a.D)[c] = v[k];
+        } else if (a.grad_tokens) {
+          reinterpret_cast<u32x4*>(static_cast<uint16_t*>(a.grad_tokens) + (base + row) * a.D)[c] = u32x4{0u, 0u, 0u, 0u};
         }
-      } else if (a.grad_tokens) {
-        u32x4* dst = reinterpret_cast<u32x4*>(static_cast<uint16_t*>(a.grad_tokens) + (base + i) * a.D);
-        for (int c = lane; c < a.D / 8; c += kWave) dst[c] = u32x4{0u, 0u, 0u, 0u};
       }
     }
   }
