@@ -89,6 +89,7 @@ class MaeLossDesc(C.Structure):
 
 
 class MaeEmbedDesc(C.Structure):
+    tensors = ()  # what it points to (make_embed_desc)
     _fields_ = [
         ("M", C.c_int64),
         ("D", C.c_int32),
@@ -104,6 +105,7 @@ class MaeEmbedDesc(C.Structure):
 
 
 class MaeDropoutDesc(C.Structure):
+    device = None  # of its tensors (make_*_desc)
     _fields_ = [
         ("M", C.c_int64),
         ("D", C.c_int32),
@@ -120,6 +122,7 @@ class MaeDropoutDesc(C.Structure):
 
 
 class MaeNormDesc(C.Structure):
+    device = None  # of its tensors (make_*_desc)
     _fields_ = [
         ("M", C.c_int64),
         ("D", C.c_int32),
@@ -133,6 +136,7 @@ class MaeNormDesc(C.Structure):
 
 
 class MaeClassDesc(C.Structure):
+    device = None  # of its tensors (make_*_desc)
     _fields_ = [
         ("M", C.c_int64),
         ("D", C.c_int32),
@@ -486,6 +490,7 @@ def make_embed_desc(visible, ids_keep, weight, bias=None, pos=None, *,
     d.visible, d.weight = visible.data_ptr(), weight.data_ptr()
     d.ids_keep, d.bias, d.pos = _ptr(ids_keep), _ptr(bias), _ptr(pos)
     d.out_dtype = out_dtype
+    d.tensors = (visible, ids_keep, weight, bias, pos)  # alive as long as the descriptor
     return d
 
 
@@ -515,7 +520,7 @@ def _one_device(*tensors, stream=None):
     """Kernels run on the current device: every tensor, descriptor and the stream have to belong to it."""
     here = torch.cuda.current_device()
     for t in tensors:
-        if t is not None and t.device.index != here:
+        if t is not None and t.device is not None and t.device.index != here:
             raise ValueError(f"tensor on {t.device}, but the current device is cuda:{here}")
     if stream is not None and stream.device.index != here:
         raise ValueError(f"stream of {stream.device}, but the current device is cuda:{here}")
@@ -545,7 +550,7 @@ def mae_patch_embed_grad(desc: MaeEmbedDesc, grad_tokens, grad_weight=None, grad
     _check(grad_bias, "grad_bias", torch.float32, numel=desc.E, optional=True)
     _check(grad_pos, "grad_pos", torch.float32, numel=desc.L * desc.E, optional=True)
     _check(workspace, "workspace", optional=True)
-    _one_device(grad_tokens, grad_weight, grad_bias, grad_pos, workspace, stream=stream)
+    _one_device(grad_tokens, grad_weight, grad_bias, grad_pos, workspace, *desc.tensors, stream=stream)
     rc = load().mae_patch_embed_grad(C.byref(desc), _ptr(grad_tokens), _ptr(grad_weight),
                                      _ptr(grad_bias), _ptr(grad_pos), _ptr(workspace),
                                      _bytes_of(workspace), _stream(stream))

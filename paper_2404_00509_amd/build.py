@@ -4,6 +4,8 @@ from __future__ import annotations
 import os
 import subprocess
 import sys
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(_HERE, "csrc")
@@ -19,9 +21,7 @@ HIPCC_FLAGS = [
 ]
 
 
-def build_hip(verbose: bool = False) -> str:
-    hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
-    cmd = [hipcc] + HIPCC_FLAGS + ["-o", OUT] + [os.path.join(CSRC, s) for s in SOURCES]
+def _run(cmd, verbose: bool) -> None:
     if verbose:
         print(" ".join(cmd), flush=True)
     res = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
@@ -30,7 +30,23 @@ def build_hip(verbose: bool = False) -> str:
     if res.returncode != 0:
         raise RuntimeError("hipcc failed:\n" + log)
     if verbose and log.strip():
-        print(log)
+        print(log, flush=True)
+
+
+def build_hip(verbose: bool = False) -> str:
+    """The sources side by side, then one link (one after the other they take four times as long)."""
+    hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
+    compile_flags = [f for f in HIPCC_FLAGS if f != "-shared"]
+    jobs = max(1, min(8, os.cpu_count() or 1, int(os.environ.get("MAX_JOBS", "8") or 8)))
+    with tempfile.TemporaryDirectory() as tmp, ThreadPoolExecutor(jobs) as pool:
+        objects = [os.path.join(tmp, s + ".o") for s in SOURCES]
+        # (the longest first)
+        order = sorted(range(len(SOURCES)), key=lambda i: -os.path.getsize(os.path.join(CSRC, SOURCES[i])))
+        todo = [pool.submit(_run, [hipcc] + compile_flags + ["-c", os.path.join(CSRC, SOURCES[i]), "-o", objects[i]],
+                            verbose) for i in order]
+        for t in todo:
+            t.result()
+        _run([hipcc] + HIPCC_FLAGS + ["-o", OUT] + objects, verbose)
     return OUT
 
 
