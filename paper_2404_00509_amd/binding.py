@@ -534,6 +534,14 @@ def _device_of(*tensors):
     return devices.pop()
 
 
+def _field(value, name, bits=31):
+    """A count or key for a field of the descriptor: ctypes would keep the low bits of a larger one."""
+    value = int(value)
+    if not 0 <= value < 1 << bits:
+        raise ValueError(f"{name} = {value}, expected 0 <= {name} < 2^{bits}")
+    return value
+
+
 def _bytes_of(t):
     return 0 if t is None else t.numel() * t.element_size()
 
@@ -567,11 +575,12 @@ def make_dropout_desc(x, residual=None, *, p, rows_per_draw=0, seed=0, batch_ind
         raise ValueError("x must have shape [..., D]")
     _check(residual, "residual", x.dtype, numel=x.numel(), optional=True)
     d = MaeDropoutDesc()
-    d.D = int(x.shape[-1])
+    d.D = _field(x.shape[-1], "D")
     d.M = x.numel() // d.D
     d.x, d.residual, d.dtype = x.data_ptr(), _ptr(residual), _mae_dtype(x)
-    d.p, d.rows_per_draw = p, rows_per_draw
-    d.seed, d.batch_index, d.layer, d.row_base = seed, batch_index, layer, row_base
+    d.p, d.rows_per_draw = p, _field(rows_per_draw, "rows_per_draw")
+    d.seed, d.batch_index = seed, batch_index
+    d.layer, d.row_base = _field(layer, "layer", 32), _field(row_base, "row_base", 64)
     d.tensors = (x, residual)
     d.device = _device_of(x, residual)
     return d
@@ -594,7 +603,7 @@ def make_norm_desc(x, weight=None, bias=None, *, eps=1e-6, y_dtype=None) -> MaeN
     _check(weight, "weight", torch.float32, numel=int(x.shape[-1]), optional=True)
     _check(bias, "bias", torch.float32, numel=int(x.shape[-1]), optional=True)
     d = MaeNormDesc()
-    d.D = int(x.shape[-1])
+    d.D = _field(x.shape[-1], "D")
     d.M = x.numel() // d.D
     d.x, d.weight, d.bias, d.eps = x.data_ptr(), _ptr(weight), _ptr(bias), eps
     d.x_dtype = _mae_dtype(x)
@@ -647,7 +656,7 @@ def make_class_desc(tokens, labels, weight, bias=None, *, smoothing=0.0,
     if tokens.shape[-1] < 1:
         raise ValueError("tokens must have shape [..., D]")
     d = MaeClassDesc()
-    d.D, d.V = int(weight.shape[1]), int(weight.shape[0])
+    d.D, d.V = _field(weight.shape[1], "D"), _field(weight.shape[0], "V")
     d.M = tokens.numel() // d.D
     _check(labels, "labels", torch.int32, numel=d.M)
     _check(bias, "bias", torch.float32, numel=d.V, optional=True)

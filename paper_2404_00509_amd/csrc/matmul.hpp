@@ -76,7 +76,8 @@ __device__ static inline const char* uniform(const uint16_t* p) {
 
 // Tiles in the order in which workgroups take them: the rows of the grid of tiles in groups of kGroup, column by
 // column within a group, so that the 32 tiles that an XCD works on at a time share kGroup panels of one operand and
-// few of the other.
+// few of the other.  (A linear loss and its gradients of 8184 rows and 32003 classes of 1024 values, on one card: 2 panels
+// 3.74 ms, 4 and 8 3.73, 6 3.74, 16 3.76: the loads come early enough for any of them.)
 constexpr uint32_t kGroup = 8;
 __device__ static inline void grouped(uint32_t id, uint32_t rows, uint32_t cols, uint32_t* row, uint32_t* col) {
   const uint32_t group = id / (kGroup * cols);

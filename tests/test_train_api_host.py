@@ -189,3 +189,25 @@ def test_binding_refuses_another_device(monkeypatch):
     here = Elsewhere()
     here.device = torch.device("cuda", 0)
     bi._one_device(here, None, stream=here)
+
+
+def test_binding_refuses_counts_that_a_field_would_cut_off(monkeypatch):
+    monkeypatch.setattr(bi, "_check", lambda *a, **k: None)
+    wide = torch.empty(1, (1 << 32) + 8, dtype=torch.bfloat16, device="meta")  # the low 32 bits say 8
+    tall = torch.empty((1 << 32) + 8, 8, dtype=torch.bfloat16, device="meta")
+    labels = torch.empty(1, dtype=torch.int32, device="meta")
+    rows = torch.empty(4, 8, dtype=torch.bfloat16, device="meta")
+    with pytest.raises(ValueError, match="D = 4294967304"):
+        mae.make_norm_desc(wide)
+    with pytest.raises(ValueError, match="D = 4294967304"):
+        mae.make_dropout_desc(wide, p=0.1)
+    with pytest.raises(ValueError, match="D = 4294967304"):
+        mae.make_class_desc(wide, labels, wide)
+    with pytest.raises(ValueError, match="V = 4294967304"):
+        mae.make_class_desc(rows, labels, tall)
+    for over in (dict(rows_per_draw=1 << 32), dict(rows_per_draw=-1), dict(layer=1 << 32), dict(layer=-1),
+                 dict(row_base=-1), dict(row_base=1 << 64)):
+        with pytest.raises(ValueError, match=next(iter(over))):
+            mae.make_dropout_desc(rows, p=0.1, **over)
+    d = mae.make_dropout_desc(rows, p=0.1, rows_per_draw=(1 << 31) - 1, layer=(1 << 32) - 1, row_base=1 << 48)
+    assert (d.rows_per_draw, d.layer, d.row_base) == ((1 << 31) - 1, (1 << 32) - 1, 1 << 48)
