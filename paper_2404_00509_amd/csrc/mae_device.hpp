@@ -45,9 +45,8 @@ __host__ __device__ inline uint64_t batch_key(uint64_t seed, uint64_t batch_inde
 
 enum Stream : uint32_t {
   kScale = 0, kRatio = 1, kTop = 2, kLeft = 3, kFlip = 4, kNoise = 5,
-  kAugOp = 6, kBlurSigma = 7, kBrightness = 8, kContrast = 9, kSaturation = 10,
-  kDropout = 11
-};
+  kAugOp = 6, kBlurSigma = 7, kBrightness = 8, kContrast = 9, kSaturation = 10
+};  // 11: kDropout, mae_kernels.hpp
 
 __device__ inline uint64_t draw(uint64_t key1, uint32_t sample, uint32_t stream, uint32_t ctr) {
   uint64_t w = ((uint64_t)sample << 32) | ((uint64_t)stream << 24) | (uint64_t)ctr;

@@ -263,6 +263,7 @@ hipError_t launch_layer_norm(const NormArgs& a, hipStream_t stream);
 hipError_t launch_layer_norm_grad(const NormArgs& a, hipStream_t stream);
 
 // ---- dropout from the keyed draws --------------------------------------------------------------------
+constexpr uint32_t kDropout = 11;  // stream number of its draws, behind those of enum Stream (mae_device.hpp)
 struct DropoutArgs {
   int64_t count;       // values
   uint64_t key;        // of the call's draws
