@@ -161,7 +161,7 @@ int mae_dropout(const mae_dropout_desc* d, void* y, void* hip_stream) {
 
 size_t mae_class_loss_workspace_bytes(const mae_class_desc* d, int32_t with_grad) {
   if (validate_class(d) != MAE_OK) return 0;
-  return mae::class_plan(d->M, d->D, d->V, d->smoothing > 0.0f, with_grad != 0).bytes;
+  return mae::class_plan(d->M, d->D, d->V, d->bias != nullptr, d->smoothing > 0.0f, with_grad != 0).bytes;
 }
 
 int mae_class_loss(const mae_class_desc* d, float* loss, float* row_loss, void* grad_tokens, void* grad_weight,
@@ -174,7 +174,7 @@ int mae_class_loss(const mae_class_desc* d, float* loss, float* row_loss, void* 
       !aligned(grad_bias, 4))
     return MAE_ERR_RANGE;
   const bool grad = grad_tokens || grad_weight || grad_bias;
-  const mae::ClassPlan p = mae::class_plan(d->M, d->D, d->V, d->smoothing > 0.0f, grad);
+  const mae::ClassPlan p = mae::class_plan(d->M, d->D, d->V, d->bias != nullptr, d->smoothing > 0.0f, grad);
   if (!has_workspace(workspace, workspace_bytes, p.bytes)) return MAE_ERR_WORKSPACE;
   rc = have_device();
   if (rc != MAE_OK) return rc;
@@ -215,6 +215,8 @@ int mae_class_loss(const mae_class_desc* d, float* loss, float* row_loss, void* 
     a.half_tokens = at(p.half_tokens, (uint16_t*)nullptr);
     a.half_weight = at(p.half_weight, (uint16_t*)nullptr);
     a.g = at(p.g, (uint16_t*)nullptr);
+    a.logits = at(p.logits, (float*)nullptr);
+    a.tops = at(p.tops, (float*)nullptr);
     a.column_sums = at(p.column_sums, (float*)nullptr);
     a.tokens_acc = at(p.tokens_acc, (float*)nullptr);
     a.weight_acc = at(p.weight_acc, (float*)nullptr);

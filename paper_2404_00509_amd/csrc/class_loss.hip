@@ -53,6 +53,8 @@ typedef int32_t i32x4_a4 __attribute__((ext_vector_type(4), aligned(4)));
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kNegInf = -__builtin_inff();
 constexpr float kGScale = 32768.0f;  // of g as fp16
+// What stats leaves of the first piece for its gradient
+enum Keep { kKeepNone, kKeepLogits, kKeepExp };
 
 // exp(v) for v <= 0
 __device__ inline float exp_neg(float v) { return __builtin_amdgcn_exp2f(v * kLog2e); }
@@ -259,9 +261,59 @@ struct Logits : Tile<TM, TN, WGM, WGN, true, true> {
   __device__ static inline uint32_t tiles(int count, int classes) {
     return (uint32_t)((count + Base::BN - 1) / Base::BN) * (uint32_t)((classes + Base::BM - 1) / Base::BM);
   }
+
+  // The tile's logits to memory or back, as they lie in the lanes.
+  template <bool kStore>
+  __device__ static inline void logits_of(const ClassArgs& a, const Place& at, int wave, int lane, f32x16 (&acc)[TM][TN]) {
+    const int64_t tile = (int64_t)at.tn * a.stat_tiles + at.tv;
+    f32x4* p = reinterpret_cast<f32x4*>(a.logits) + (tile * (WGM * WGN) + wave) * (TM * TN * 4 * kWave) + lane;
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+      for (int j = 0; j < TN; ++j)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          f32x4* to = p + ((i * TN + j) * 4 + q) * kWave;
+          if (kStore) {
+            *to = f32x4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+          } else {
+            const f32x4 v = *to;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) acc[i][j][4 * q + k] = v[k];
+          }
+        }
+  }
+
+  static constexpr int kPitch = 32 * TM + 8;  // of a wavefront's strip of 32 rows, in fp16
+  static constexpr int kStripBytes = WGM * WGN * 32 * kPitch * 2;
+  // Rows 32 j .. + 31 of a wavefront's values as fp16 to g, through its strip of LDS: 16 bytes per lane along a row.
+  template <int j>
+  __device__ static inline void store_block(const ClassArgs& a, const Place& at, int wave, int lane,
+                                            const f32x16 (&acc)[TM][TN], uint16_t* strip) {
+    const int wm = wave / WGN, wn = wave % WGN, half = 4 * (lane >> 5);
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        *reinterpret_cast<u32x2*>(strip + (lane & 31) * kPitch + 32 * i + 8 * q + half) =
+            u32x2{half_pair(acc[i][j][4 * q], acc[i][j][4 * q + 1]), half_pair(acc[i][j][4 * q + 2], acc[i][j][4 * q + 3])};
+    __builtin_amdgcn_wave_barrier();
+    constexpr int kLanesPerRow = 4 * TM, kRowsPerRep = kWave / kLanesPerRow;
+#pragma unroll
+    for (int rep = 0; rep < 32 / kRowsPerRep; ++rep) {
+      const int sr = rep * kRowsPerRep + lane / kLanesPerRow;
+      const int col = (lane % kLanesPerRow) * 8;
+      const u32x4 v = *reinterpret_cast<const u32x4*>(strip + sr * kPitch + col);
+      const int row = wn * 32 * TN + j * 32 + sr;
+      const int c = at.c0 + wm * 32 * TM + col;
+      if (row < at.rows_n && c < a.piece_ld)
+        *reinterpret_cast<u32x4*>(a.g + (at.n0 + row) * (int64_t)a.piece_ld + c) = v;
+    }
+    __builtin_amdgcn_wave_barrier();
+  }
 };
 
-template <int TM, int TN, int WGM, int WGN>
+template <int TM, int TN, int WGM, int WGN, int kKeep>
 __global__ __launch_bounds__(64 * WGM * WGN) void class_stats_kernel(ClassArgs a) {
   using T = Logits<TM, TN, WGM, WGN>;
   __shared__ __attribute__((aligned(1024))) u32x4 lds[T::kLdsBytes / 16];
@@ -270,28 +322,32 @@ __global__ __launch_bounds__(64 * WGM * WGN) void class_stats_kernel(ClassArgs a
   if (blockIdx.x >= tiles) return;
   const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
   const int wm = wave / WGN, wn = wave % WGN;
-  // beside the epilogue of a tile the next one's first slices are brought in; the epilogue has the ring's last place
-  float* part = reinterpret_cast<float*>(lds + 4 * T::kSlots);  // [WGM][BN][3]
-  static_assert(WGM * T::BN * 3 * 4 <= T::kPlaceBytes, "room in a place");
+  // beside the epilogue of a tile the next one's first slices are brought in; the epilogue has the ring's other places
+  constexpr int kAhead = kKeep == kKeepExp ? 2 : 4;
+  constexpr int kStrips = kKeep == kKeepExp ? T::kStripBytes : 0;
+  char* room = reinterpret_cast<char*>(lds + kAhead * T::kSlots);
+  float* part = reinterpret_cast<float*>(room + kStrips);  // [WGM][BN][3]
+  static_assert(kStrips + WGM * T::BN * 3 * 4 <= (T::kPlaces - kAhead) * T::kPlaceBytes, "room in the places");
   typename T::Place next = T::place(a, blockIdx.x, tiles, count, 0, a.V);
-  T::template fill<0, 4>(next.source, lds);
+  T::template fill<0, kAhead>(next.source, lds);
   for (uint32_t id = blockIdx.x; id < tiles; id += gridDim.x) {
     const typename T::Place at = next;
     f32x16 acc[TM][TN];
-    T::template run<4>(at.source, lds, acc);
+    T::template run<kAhead>(at.source, lds, acc);
     const int v0 = at.c0, rows_v = at.rows_v, rows_n = at.rows_n;
     const int64_t n0 = at.n0;
     const int first = v0 + wm * 32 * TM;
     __syncthreads();  // every wavefront is done with the ring
     if (id + gridDim.x < tiles) {
       next = T::place(a, id + gridDim.x, tiles, count, 0, a.V);
-      T::template fill<0, 4>(next.source, lds);
+      T::template fill<0, kAhead>(next.source, lds);
     }
     add_bias<TM, TN>(a.bias, first, a.V, lane, acc);
+    if (kKeep == kKeepLogits) T::template logits_of<true>(a, at, wave, lane, acc);
     const int half = 4 * (lane >> 5);
     const int classes = a.V - first - half;  // class 32 i + 8 (e / 4) + e % 4 of this lane exists if below
-#pragma unroll
-    for (int j = 0; j < TN; ++j) {
+    unroll<TN>([&](auto j_tag) {
+      constexpr int j = decltype(j_tag)::value;
       const int r = wn * 32 * TN + j * 32 + (lane & 31);
       const int y = r < rows_n ? a.label_of[n0 + r] - first - half : -1;
       float sl = 0.f;
@@ -328,7 +384,11 @@ __global__ __launch_bounds__(64 * WGM * WGN) void class_stats_kernel(ClassArgs a
 #pragma unroll
       for (int i = 0; i < TM; ++i)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) s += exp_neg(acc[i][j][e] - from);
+        for (int e = 0; e < 16; ++e) {
+          const float v = exp_neg(acc[i][j][e] - from);
+          s += v;
+          if (kKeep == kKeepExp) acc[i][j][e] = v * kGScale;
+        }
       s += __shfl_xor(s, 32, kWave);
       sl += __shfl_xor(sl, 32, kWave);
       if (lane < 32) {
@@ -337,7 +397,11 @@ __global__ __launch_bounds__(64 * WGM * WGN) void class_stats_kernel(ClassArgs a
         p[1] = s;
         p[2] = sl;
       }
-    }
+      if (kKeep == kKeepExp && v0 < a.piece_classes) {  // (pieces are whole tiles, or all classes)
+        if (lane < 32 && r < rows_n) a.tops[(n0 + r) * (int64_t)a.top_ld + at.tv * WGM + wm] = m;
+        T::template store_block<j>(a, at, wave, lane, acc, reinterpret_cast<uint16_t*>(room) + wave * 32 * T::kPitch);
+      }
+    });
     __syncthreads();
     for (int r = tid; r < rows_n; r += T::kThreads) {
       float m = kNegInf, s = 0.f, sl = 0.f;
@@ -501,13 +565,14 @@ __device__ inline void halve(float* v, int lane) {
   }
 }
 
-template <int TM, int TN, int WGM, int WGN>
+// kKept: from the logits that stats has kept (of all classes), a tile per workgroup.
+template <int TM, int TN, int WGM, int WGN, bool kKept>
 __global__ __launch_bounds__(64 * WGM * WGN) void class_grad_kernel(ClassArgs a) {
   using T = Logits<TM, TN, WGM, WGN>;
-  constexpr int kPitch = 32 * TM + 8;  // of a wavefront's strip of 32 rows, in fp16
-  constexpr int kStripBytes = WGM * WGN * 32 * kPitch * 2;
-  static_assert(kStripBytes + WGN * T::BM * 4 <= 3 * T::kPlaceBytes, "room in three places");
-  __shared__ __attribute__((aligned(1024))) u32x4 lds[T::kLdsBytes / 16];
+  // beside the epilogue of a tile the next one's first slice is brought in; the epilogue has the ring's last three places
+  constexpr int kRoomBytes = T::kStripBytes + WGN * T::BM * 4;
+  static_assert(kRoomBytes <= 3 * T::kPlaceBytes, "room in three places");
+  __shared__ __attribute__((aligned(1024))) u32x4 lds[(kKept ? kRoomBytes : T::kLdsBytes) / 16];
   const int count = uniform(*a.count);
   const uint32_t tiles = T::tiles(count, a.piece_classes);
   // (with the first piece: the loss, by a workgroup that has no more tiles than any other)
@@ -515,31 +580,33 @@ __global__ __launch_bounds__(64 * WGM * WGN) void class_grad_kernel(ClassArgs a)
   if (blockIdx.x >= tiles) return;
   const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
   const int wm = wave / WGN, wn = wave % WGN;
-  // beside the epilogue of a tile the next one's first slice is brought in; the epilogue has the ring's last three places
-  char* room = reinterpret_cast<char*>(lds + 2 * T::kSlots);
-  uint16_t* strip = reinterpret_cast<uint16_t*>(room) + wave * 32 * kPitch;
-  float* columns = reinterpret_cast<float*>(room + kStripBytes);
+  char* room = reinterpret_cast<char*>(lds + (kKept ? 0 : 2 * T::kSlots));
+  uint16_t* strip = reinterpret_cast<uint16_t*>(room) + wave * 32 * T::kPitch;
+  float* columns = reinterpret_cast<float*>(room + T::kStripBytes);
   typename T::Place next = T::place(a, blockIdx.x, tiles, count, a.piece_first, a.piece_classes);
-  T::template fill<0, 2>(next.source, lds);
+  if (!kKept) T::template fill<0, 2>(next.source, lds);
   for (uint32_t id = blockIdx.x; id < tiles; id += gridDim.x) {
     const typename T::Place at = next;
     f32x16 acc[TM][TN];
-    T::template run<2>(at.source, lds, acc);
+    if constexpr (kKept) T::template logits_of<false>(a, at, wave, lane, acc);
+    else T::template run<2>(at.source, lds, acc);
     const int c0 = at.c0, rows_v = at.rows_v, rows_n = at.rows_n;
     const int64_t n0 = at.n0;
     const int first = a.piece_first + c0 + wm * 32 * TM;
-    __syncthreads();  // every wavefront is done with the ring
-    if (id + gridDim.x < tiles) {
-      next = T::place(a, id + gridDim.x, tiles, count, a.piece_first, a.piece_classes);
-      T::template fill<0, 2>(next.source, lds);
+    if constexpr (!kKept) {
+      __syncthreads();  // every wavefront is done with the ring
+      if (id + gridDim.x < tiles) {
+        next = T::place(a, id + gridDim.x, tiles, count, a.piece_first, a.piece_classes);
+        T::template fill<0, 2>(next.source, lds);
+      }
+      add_bias<TM, TN>(a.bias, first, a.V, lane, acc);
     }
-    add_bias<TM, TN>(a.bias, first, a.V, lane, acc);
 
     const float uniform = a.smoothing / (float)a.V * kGScale, label = (1.0f - a.smoothing) * kGScale;
     const int half = 4 * (lane >> 5);
     const int classes = a.piece_first + a.piece_classes - first - half;  // of the piece, from this lane's first one on
-#pragma unroll
-    for (int j = 0; j < TN; ++j) {
+    unroll<TN>([&](auto j_tag) {
+      constexpr int j = decltype(j_tag)::value;
       const int r = wn * 32 * TN + j * 32 + (lane & 31);
       const bool live = r < rows_n;  // (a row that does not exist gets zeros)
       const float m = live ? a.row_max[n0 + r] : __builtin_inff(), inv = live ? a.row_inv[n0 + r] * kGScale : 0.f;
@@ -561,28 +628,8 @@ __global__ __launch_bounds__(64 * WGM * WGN) void class_grad_kernel(ClassArgs a)
 #pragma unroll
           for (int e = 0; e < 16; ++e) acc[i][j][e] = 32 * i + 8 * (e >> 2) + (e & 3) < classes ? acc[i][j][e] : 0.f;
       }
-#pragma unroll
-      for (int i = 0; i < TM; ++i)
-#pragma unroll
-        for (int q = 0; q < 4; ++q)
-          *reinterpret_cast<u32x2*>(strip + (lane & 31) * kPitch + 32 * i + 8 * q + half) =
-              u32x2{half_pair(acc[i][j][4 * q], acc[i][j][4 * q + 1]), half_pair(acc[i][j][4 * q + 2], acc[i][j][4 * q + 3])};
-      __builtin_amdgcn_wave_barrier();
-      // rows of the strip to memory, 16 bytes per lane
-      constexpr int kLanesPerRow = 4 * TM;
-      constexpr int kRowsPerRep = kWave / kLanesPerRow;
-#pragma unroll
-      for (int rep = 0; rep < 32 / kRowsPerRep; ++rep) {
-        const int sr = rep * kRowsPerRep + lane / kLanesPerRow;
-        const int col = (lane % kLanesPerRow) * 8;
-        const u32x4 v = *reinterpret_cast<const u32x4*>(strip + sr * kPitch + col);
-        const int row = wn * 32 * TN + j * 32 + sr;
-        const int c = c0 + wm * 32 * TM + col;
-        if (row < rows_n && c < a.piece_ld)
-          *reinterpret_cast<u32x4*>(a.g + (n0 + row) * (int64_t)a.piece_ld + c) = v;
-      }
-      __builtin_amdgcn_wave_barrier();
-    }
+      T::template store_block<j>(a, at, wave, lane, acc, strip);
+    });
     if (a.column_sums) {
       // sums over the tile's rows: over j in registers, over 32 lanes by halving, over wavefronts through LDS
       float v[16 * TM];
@@ -628,6 +675,46 @@ __global__ __launch_bounds__(64 * WGM * WGN) void class_grad_kernel(ClassArgs a)
       }
     }
     __syncthreads();
+  }
+}
+
+// ---- the same from the exponentials that stats has kept of the first piece ------------------------------------
+// A workgroup: kKeptRows rows by 256 classes, eight classes of every eighth row per lane.
+constexpr int kKeptThreads = 256, kKeptColumns = 256, kKeptRows = 32;
+__global__ __launch_bounds__(kKeptThreads) void class_kept_kernel(ClassArgs a) {
+  constexpr int kLanesPerRow = kKeptColumns / 8, kStep = kKeptThreads / kLanesPerRow, kTurns = kKeptRows / kStep;
+  __shared__ double sums[kRowWaves];
+  if (blockIdx.x == gridDim.x - 1) join_losses(a, sums);
+  const int count = uniform(*a.count);
+  const uint32_t chunks = (uint32_t)((a.piece_classes + kKeptColumns - 1) / kKeptColumns);
+  const int64_t row0 = (int64_t)(blockIdx.x / chunks) * kKeptRows + (int)threadIdx.x / kLanesPerRow;
+  const int c = (int)(blockIdx.x % chunks) * kKeptColumns + (int)(threadIdx.x % kLanesPerRow) * 8;
+  if (row0 >= count || c >= a.piece_ld) return;
+  const float off = a.smoothing / (float)a.V * kGScale, label = (1.0f - a.smoothing) * kGScale;
+  f16x8 e[kTurns];
+#pragma unroll
+  for (int t = 0; t < kTurns; ++t)
+    if (row0 + t * kStep < count) e[t] = *reinterpret_cast<const f16x8*>(a.g + (row0 + t * kStep) * a.piece_ld + c);
+#pragma unroll
+  for (int t = 0; t < kTurns; ++t) {
+    const int64_t row = row0 + t * kStep;
+    if (row >= count) break;
+    const float m = a.row_max[row], inv = a.row_inv[row];
+    const int y = a.label_of[row] - c;
+    const float scale = exp_neg(a.tops[row * a.top_ld + c / a.top_classes] - m) * inv;
+    float v[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = (float)e[t][k] * scale - off;
+    if (y >= 0 && y < 8) {  // (the label's anew from its logit: what is left of 1 - exp / sum has no digits to lose)
+      const float own = exp_neg(a.label_logit[row] - m) * (inv * kGScale) - off - label;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[k] = k == y ? own : v[k];
+    }
+    u32x4 out;
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      out[k] = half_pair(c + 2 * k < a.piece_classes ? v[2 * k] : 0.f, c + 2 * k + 1 < a.piece_classes ? v[2 * k + 1] : 0.f);
+    *reinterpret_cast<u32x4*>(a.g + row * a.piece_ld + c) = out;
   }
 }
 
@@ -825,7 +912,12 @@ static int products_side(int64_t M, int D, int V) {
   return M <= 256 || tiles(256) < 256 ? 128 : 256;
 }
 
-ClassPlan class_plan(int64_t M, int D, int V, bool smooth, bool grad) {
+// What stats keeps for the gradient, so that the logits need not be made again: all logits in fp32 where they fit the
+// caches (64 MiB); else, if there is no gradient of a bias, which is to have single precision, the exponentials of the first
+// piece in the place of its g.
+constexpr int64_t kMostLogits = int64_t(1) << 24;
+
+ClassPlan class_plan(int64_t M, int D, int V, bool bias, bool smooth, bool grad) {
   ClassPlan p{};
   p.few = !grad && M <= kFewRows;
   p.side = logits_side(M, V);
@@ -850,11 +942,16 @@ ClassPlan class_plan(int64_t M, int D, int V, bool smooth, bool grad) {
     p.partials = take((size_t)p.row_blocks * 8);
   }
   if (grad) {
-    // g of a piece takes at most 512 MiB, or 1024 classes
-    const int64_t most = (int64_t(1) << 28) / M / 256 * 256;
+    // g of a piece takes at most 1 GiB, or 1024 classes
+    const int64_t most = (int64_t(1) << 29) / M / 256 * 256;
     p.piece = (int)(most < 1024 ? 1024 : most < V ? most : V);
     if (p.piece > V) p.piece = V;
     p.piece_ld = (int)ceil_div(p.piece, 64) * 64;
+    const int64_t padded = ceil_div(M, p.side) * ceil_div(V, p.side) * p.side * p.side;
+    p.keep = padded <= kMostLogits ? kKeepLogits : bias ? kKeepNone : kKeepExp;
+    p.top_ld = (int)ceil_div(p.piece, p.side) * 2;
+    p.logits = take(p.keep == kKeepLogits ? (size_t)padded * 4 : 0);
+    p.tops = take(p.keep == kKeepExp ? m * p.top_ld * 4 : 0);
     p.products_side = products_side(M, D, p.piece);
     // (the tiles for grad_weight alone fill the compute units: the others, in the same launch, are split less)
     const bool many = ceil_div(p.piece, p.products_side) * ceil_div(D, p.products_side) >= 256;
@@ -869,7 +966,7 @@ ClassPlan class_plan(int64_t M, int D, int V, bool smooth, bool grad) {
     p.half_tokens = take(m * D * 2);
     p.half_weight = take((size_t)V * D * 2);
     p.g = take(m * p.piece_ld * 2);
-    p.column_sums = take((size_t)ceil_div(M, p.side) * p.piece * 4);
+    p.column_sums = take(bias ? (size_t)ceil_div(M, p.side) * p.piece * 4 : 0);
     if (p.tokens_parts > 1 || p.piece < V) p.tokens_acc = take(m * D * 4 * p.tokens_parts);
     if (p.weight_parts > 1) p.weight_acc = take((size_t)p.piece * D * 4 * p.weight_parts);
   }
@@ -886,15 +983,27 @@ uint32_t walkers(int64_t M, int classes) {
   return (uint32_t)(tiles < 256 * kPerUnit ? tiles : 256 * kPerUnit);
 }
 template <int TM, int TN, int WGM, int WGN>
-void launch_stats(const ClassArgs& a, hipStream_t stream) {
+void launch_stats(const ClassArgs& a, int keep, hipStream_t stream) {
   using T = Logits<TM, TN, WGM, WGN>;
-  hipLaunchKernelGGL((class_stats_kernel<TM, TN, WGM, WGN>), dim3(walkers<T>(a.M, a.V)), dim3(T::kThreads), 0, stream, a);
+  const dim3 grid(walkers<T>(a.M, a.V)), block(T::kThreads);
+  if (keep == kKeepLogits) hipLaunchKernelGGL((class_stats_kernel<TM, TN, WGM, WGN, kKeepLogits>), grid, block, 0, stream, a);
+  else if (keep == kKeepExp) hipLaunchKernelGGL((class_stats_kernel<TM, TN, WGM, WGN, kKeepExp>), grid, block, 0, stream, a);
+  else hipLaunchKernelGGL((class_stats_kernel<TM, TN, WGM, WGN, kKeepNone>), grid, block, 0, stream, a);
+}
+void launch_kept(const ClassArgs& a, hipStream_t stream) {
+  hipLaunchKernelGGL(class_kept_kernel, dim3((uint32_t)(ceil_div(a.M, kKeptRows) * ceil_div(a.piece_classes, kKeptColumns))),
+                     dim3(kKeptThreads), 0, stream, a);
 }
 template <int TM, int TN, int WGM, int WGN>
-void launch_grad(const ClassArgs& a, hipStream_t stream) {
+void launch_grad(const ClassArgs& a, int keep, hipStream_t stream) {
   using T = Logits<TM, TN, WGM, WGN>;
-  hipLaunchKernelGGL((class_grad_kernel<TM, TN, WGM, WGN>), dim3(walkers<T>(a.M, a.piece_classes)), dim3(T::kThreads), 0,
-                     stream, a);
+  if (keep == kKeepLogits) {
+    const dim3 grid((uint32_t)(ceil_div(a.M, T::BN) * ceil_div(a.V, T::BM)));
+    hipLaunchKernelGGL((class_grad_kernel<TM, TN, WGM, WGN, true>), grid, dim3(T::kThreads), 0, stream, a);
+  } else {
+    hipLaunchKernelGGL((class_grad_kernel<TM, TN, WGM, WGN, false>), dim3(walkers<T>(a.M, a.piece_classes)),
+                       dim3(T::kThreads), 0, stream, a);
+  }
 }
 template <int TM, int TN, int WGM, int WGN>
 void launch_products(const ClassArgs& a, const Product& tokens, const Product& weight, hipStream_t stream) {
@@ -922,9 +1031,14 @@ hipError_t launch_class_loss(ClassArgs a, const ClassPlan& p, hipStream_t stream
   if (!p.few)
     hipLaunchKernelGGL(class_pack_kernel, dim3((uint32_t)(grad ? p.num_peaks : a.pack_blocks)), dim3(kPackThreads), 0,
                        stream, a);
-  if (p.side == 256) launch_stats<4, 2, 2, 4>(a, stream);
-  else if (p.side == 128) launch_stats<2, 1, 2, 4>(a, stream);
-  else launch_stats<1, 1, 2, 2>(a, stream);
+  a.piece_first = 0;
+  a.piece_classes = p.piece;
+  a.piece_ld = p.piece_ld;
+  a.top_ld = p.top_ld;
+  a.top_classes = p.side / 2;
+  if (p.side == 256) launch_stats<4, 2, 2, 4>(a, p.keep, stream);
+  else if (p.side == 128) launch_stats<2, 1, 2, 4>(a, p.keep, stream);
+  else launch_stats<1, 1, 2, 2>(a, p.keep, stream);
   if (p.few) {
     hipLaunchKernelGGL(class_few_rows_kernel, dim3(1), dim3(kFewThreads), 0, stream, a);
     return hipGetLastError();
@@ -937,7 +1051,6 @@ hipError_t launch_class_loss(ClassArgs a, const ClassPlan& p, hipStream_t stream
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !grad) return e;
 
-  a.piece_ld = p.piece_ld;
   a.grad_rows = p.side;
   a.tokens_parts = p.tokens_parts;
   a.weight_parts = p.weight_parts;
@@ -946,9 +1059,10 @@ hipError_t launch_class_loss(ClassArgs a, const ClassPlan& p, hipStream_t stream
     a.piece_first = first;
     a.piece_classes = a.V - first < p.piece ? a.V - first : p.piece;
     const bool last = first + a.piece_classes == a.V;
-    if (p.side == 256) launch_grad<4, 2, 2, 4>(a, stream);
-    else if (p.side == 128) launch_grad<2, 1, 2, 4>(a, stream);
-    else launch_grad<1, 1, 2, 2>(a, stream);
+    if (p.keep == kKeepExp && first == 0) launch_kept(a, stream);
+    else if (p.side == 256) launch_grad<4, 2, 2, 4>(a, p.keep, stream);
+    else if (p.side == 128) launch_grad<2, 1, 2, 4>(a, p.keep, stream);
+    else launch_grad<1, 1, 2, 2>(a, p.keep, stream);
     Product tokens{}, weight{};
     if (a.grad_tokens) {
       // rows: packed rows; k: classes of the piece (g holds zeros up to a multiple of 8 behind them)

@@ -285,14 +285,15 @@ struct ClassPlan {
   int side;                           // of the tiles of logits
   int stat_tiles, pack_rows, row_blocks;
   int piece, piece_ld;                // classes per piece of the gradient; row length of g
+  int keep, top_ld;                   // what stats leaves for the gradient; row length of tops
   int products_side, tokens_parts, weight_parts;  // of the products for grad_tokens and grad_weight
   int num_peaks, num_weight_peaks;    // workgroups of the first kernel; of them, those that look at the weight
   // places in the workspace
   size_t stats, logit_sums, label_logit, count, label_of, row_of, packed, partials;
-  size_t peaks, row_max, row_inv, half_tokens, half_weight, g, column_sums, tokens_acc, weight_acc;
+  size_t peaks, row_max, row_inv, half_tokens, half_weight, g, column_sums, tokens_acc, weight_acc, logits, tops;
   size_t bytes;
 };
-ClassPlan class_plan(int64_t M, int D, int V, bool smooth, bool grad);
+ClassPlan class_plan(int64_t M, int D, int V, bool bias, bool smooth, bool grad);
 struct ClassArgs {
   int64_t M;
   int32_t D, V;
@@ -321,12 +322,15 @@ struct ClassArgs {
   uint16_t* half_tokens;  // [slot][D] fp16, scaled by a power of two
   uint16_t* half_weight;  // [V][D]
   uint16_t* g;            // [slot][piece_ld] fp16, times 2^15
+  float* logits;          // [tile], as they lie in the lanes, if they are kept
+  float* tops;            // [slot][top_ld] if exponentials are kept (in g): what they were taken under, per top_classes
   float* column_sums;     // [row tile][classes of the piece]
   float* tokens_acc;      // [tokens_parts][M][D]
   float* weight_acc;      // [weight_parts][classes of the piece][D]
   // filled in by the launcher
   int32_t pack_rows, stat_tiles, pack_blocks, num_peaks, row_blocks;
   int32_t piece_first, piece_classes, piece_ld, grad_rows, tokens_parts, weight_parts;
+  int32_t top_ld, top_classes;
 };
 hipError_t launch_class_loss(ClassArgs a, const ClassPlan& p, hipStream_t stream);
 

@@ -64,8 +64,39 @@ def test_sizes(M, D, V):
         _check(x, y, w, b, smoothing, what=f"M{M} D{D} V{V} bias {bias}")
 
 
+# logits kept in fp32 for the gradient up to 64 MiB, exponentials in fp16 beyond that without a bias, nothing with one; tiles
+# of all sides; the last group of classes whole, ragged and of one class
+@pytest.mark.parametrize("M,D,V", [(2048, 64, 8192), (2048, 64, 8193), (16390, 40, 1024), (17000, 8, 1000), (17, 24, 1 << 20),
+                                   (200, 72, 90_001), (60, 16, 300_000)])
+def test_what_is_kept_for_the_gradient(M, D, V):
+    for bias, smoothing, left_out in ((False, 0.1, 0.2), (True, 0.0, 0.0)):
+        x, y, w, b = _inputs(16, M, D, V, bias, left_out, 4.0)
+        _check(x, y, w, b, smoothing, -0.5, what=f"M{M} D{D} V{V} bias {bias}")
+
+
+def test_kept_exponentials_of_far_tiles_and_of_a_row_that_is_not_finite():
+    M, D, V = 2100, 64, 8300
+    x, y, w, _ = _inputs(17, M, D, V, False, spread=30.0)  # most groups of classes lie far under their row's maximum
+    clean = _check(x, y, w, None, what="far")
+    x[77, 3] = float("inf")
+    out = _run(x, y, w, None)
+    rest = torch.arange(M, device="cuda") != 77
+    assert torch.isnan(out["loss"]).all() and torch.isnan(out["grad_tokens"][77]).all()
+    assert torch.equal(out["row_loss"][rest], clean["row_loss"][rest])
+    assert torch.equal(out["grad_tokens"][rest], clean["grad_tokens"][rest])
+    none = _run(x, torch.full_like(y, -1), w, None, 0.1)
+    assert not any(bool(v.any()) for v in none.values())
+
+
+def test_vocabulary_in_pieces_without_a_bias():
+    # the first piece from what was kept, the other anew
+    M, D, V = 1 << 18, 8, 2100
+    x, y, w, b = _inputs(18, M, D, V, False, 0.2)
+    _check(x, y, w, b, 0.1, what="pieces")
+
+
 def test_vocabulary_in_pieces():
-    # the gradient goes through the classes 1024 at a time here, and the rows' labels lie in all of them
+    # the gradient goes through the classes 2048 at a time here, and the rows' labels lie in all of them
     M, D, V = 1 << 18, 8, 2100
     x, y, w, b = _inputs(2, M, D, V, True, 0.2)
     _check(x, y, w, b, 0.1, what="pieces")
