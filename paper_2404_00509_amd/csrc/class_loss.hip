@@ -284,32 +284,30 @@ struct Logits : Tile<TM, TN, WGM, WGN, true, true> {
         }
   }
 
-  static constexpr int kPitch = 32 * TM + 8;  // of a wavefront's strip of 32 rows, in fp16
-  static constexpr int kStripBytes = WGM * WGN * 32 * kPitch * 2;
-  // Rows 32 j .. + 31 of a wavefront's values as fp16 to g, through its strip of LDS: 16 bytes per lane along a row.
+  // Rows 32 j .. + 31 of a wavefront's values as fp16 to g.  A lane has every second group of four classes of its row: the
+  // halves of the wavefront swap theirs, so that each has groups of eight, 16 bytes.  (Through strips of LDS, 256
+  // bytes along a row at a time: 3 % of a call over 32,003 classes more.)
   template <int j>
   __device__ static inline void store_block(const ClassArgs& a, const Place& at, int wave, int lane,
-                                            const f32x16 (&acc)[TM][TN], uint16_t* strip) {
-    const int wm = wave / WGN, wn = wave % WGN, half = 4 * (lane >> 5);
+                                            const f32x16 (&acc)[TM][TN]) {
+    const int wm = wave / WGN, wn = wave % WGN;
+    const int row = wn * 32 * TN + j * 32 + (lane & 31), c = at.c0 + wm * 32 * TM + 8 * (lane >> 5);
+    uint16_t* to = a.g + (at.n0 + row) * (int64_t)a.piece_ld + c;
 #pragma unroll
     for (int i = 0; i < TM; ++i)
 #pragma unroll
-      for (int q = 0; q < 4; ++q)
-        *reinterpret_cast<u32x2*>(strip + (lane & 31) * kPitch + 32 * i + 8 * q + half) =
-            u32x2{half_pair(acc[i][j][4 * q], acc[i][j][4 * q + 1]), half_pair(acc[i][j][4 * q + 2], acc[i][j][4 * q + 3])};
-    __builtin_amdgcn_wave_barrier();
-    constexpr int kLanesPerRow = 4 * TM, kRowsPerRep = kWave / kLanesPerRow;
+      for (int q = 0; q < 4; q += 2) {
+        u32x4 v;
 #pragma unroll
-    for (int rep = 0; rep < 32 / kRowsPerRep; ++rep) {
-      const int sr = rep * kRowsPerRep + lane / kLanesPerRow;
-      const int col = (lane % kLanesPerRow) * 8;
-      const u32x4 v = *reinterpret_cast<const u32x4*>(strip + sr * kPitch + col);
-      const int row = wn * 32 * TN + j * 32 + sr;
-      const int c = at.c0 + wm * 32 * TM + col;
-      if (row < at.rows_n && c < a.piece_ld)
-        *reinterpret_cast<u32x4*>(a.g + (at.n0 + row) * (int64_t)a.piece_ld + c) = v;
-    }
-    __builtin_amdgcn_wave_barrier();
+        for (int k = 0; k < 2; ++k) {
+          const auto swapped = __builtin_amdgcn_permlane32_swap(
+              half_pair(acc[i][j][4 * q + 2 * k], acc[i][j][4 * q + 2 * k + 1]),
+              half_pair(acc[i][j][4 * q + 4 + 2 * k], acc[i][j][4 * q + 5 + 2 * k]), false, false);
+          v[k] = swapped[0];
+          v[2 + k] = swapped[1];
+        }
+        if (row < at.rows_n && c + 32 * i + 8 * q < a.piece_ld) *reinterpret_cast<u32x4*>(to + 32 * i + 8 * q) = v;
+      }
   }
 };
 
@@ -322,25 +320,22 @@ __global__ __launch_bounds__(64 * WGM * WGN) void class_stats_kernel(ClassArgs a
   if (blockIdx.x >= tiles) return;
   const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
   const int wm = wave / WGN, wn = wave % WGN;
-  // beside the epilogue of a tile the next one's first slices are brought in; the epilogue has the ring's other places
-  constexpr int kAhead = kKeep == kKeepExp ? 2 : 4;
-  constexpr int kStrips = kKeep == kKeepExp ? T::kStripBytes : 0;
-  char* room = reinterpret_cast<char*>(lds + kAhead * T::kSlots);
-  float* part = reinterpret_cast<float*>(room + kStrips);  // [WGM][BN][3]
-  static_assert(kStrips + WGM * T::BN * 3 * 4 <= (T::kPlaces - kAhead) * T::kPlaceBytes, "room in the places");
+  // beside the epilogue of a tile the next one's first slices are brought in; the epilogue has the ring's last place
+  float* part = reinterpret_cast<float*>(lds + 4 * T::kSlots);  // [WGM][BN][3]
+  static_assert(WGM * T::BN * 3 * 4 <= T::kPlaceBytes, "room in a place");
   typename T::Place next = T::place(a, blockIdx.x, tiles, count, 0, a.V);
-  T::template fill<0, kAhead>(next.source, lds);
+  T::template fill<0, 4>(next.source, lds);
   for (uint32_t id = blockIdx.x; id < tiles; id += gridDim.x) {
     const typename T::Place at = next;
     f32x16 acc[TM][TN];
-    T::template run<kAhead>(at.source, lds, acc);
+    T::template run<4>(at.source, lds, acc);
     const int v0 = at.c0, rows_v = at.rows_v, rows_n = at.rows_n;
     const int64_t n0 = at.n0;
     const int first = v0 + wm * 32 * TM;
     __syncthreads();  // every wavefront is done with the ring
     if (id + gridDim.x < tiles) {
       next = T::place(a, id + gridDim.x, tiles, count, 0, a.V);
-      T::template fill<0, kAhead>(next.source, lds);
+      T::template fill<0, 4>(next.source, lds);
     }
     add_bias<TM, TN>(a.bias, first, a.V, lane, acc);
     if (kKeep == kKeepLogits) T::template logits_of<true>(a, at, wave, lane, acc);
@@ -399,7 +394,7 @@ __global__ __launch_bounds__(64 * WGM * WGN) void class_stats_kernel(ClassArgs a
       }
       if (kKeep == kKeepExp && v0 < a.piece_classes) {  // (pieces are whole tiles, or all classes)
         if (lane < 32 && r < rows_n) a.tops[(n0 + r) * (int64_t)a.top_ld + at.tv * WGM + wm] = m;
-        T::template store_block<j>(a, at, wave, lane, acc, reinterpret_cast<uint16_t*>(room) + wave * 32 * T::kPitch);
+        T::template store_block<j>(a, at, wave, lane, acc);
       }
     });
     __syncthreads();
@@ -569,9 +564,9 @@ __device__ inline void halve(float* v, int lane) {
 template <int TM, int TN, int WGM, int WGN, bool kKept>
 __global__ __launch_bounds__(64 * WGM * WGN) void class_grad_kernel(ClassArgs a) {
   using T = Logits<TM, TN, WGM, WGN>;
-  // beside the epilogue of a tile the next one's first slice is brought in; the epilogue has the ring's last three places
-  constexpr int kRoomBytes = T::kStripBytes + WGN * T::BM * 4;
-  static_assert(kRoomBytes <= 3 * T::kPlaceBytes, "room in three places");
+  // beside the epilogue of a tile the next one's first slices are brought in; the epilogue has the ring's last place
+  constexpr int kRoomBytes = WGN * T::BM * 4;
+  static_assert(kRoomBytes <= T::kPlaceBytes, "room in a place");
   __shared__ __attribute__((aligned(1024))) u32x4 lds[(kKept ? kRoomBytes : T::kLdsBytes) / 16];
   const int count = uniform(*a.count);
   const uint32_t tiles = T::tiles(count, a.piece_classes);
@@ -580,16 +575,14 @@ __global__ __launch_bounds__(64 * WGM * WGN) void class_grad_kernel(ClassArgs a)
   if (blockIdx.x >= tiles) return;
   const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
   const int wm = wave / WGN, wn = wave % WGN;
-  char* room = reinterpret_cast<char*>(lds + (kKept ? 0 : 2 * T::kSlots));
-  uint16_t* strip = reinterpret_cast<uint16_t*>(room) + wave * 32 * T::kPitch;
-  float* columns = reinterpret_cast<float*>(room + T::kStripBytes);
+  float* columns = reinterpret_cast<float*>(lds + (kKept ? 0 : 4 * T::kSlots));
   typename T::Place next = T::place(a, blockIdx.x, tiles, count, a.piece_first, a.piece_classes);
-  if (!kKept) T::template fill<0, 2>(next.source, lds);
+  if (!kKept) T::template fill<0, 4>(next.source, lds);
   for (uint32_t id = blockIdx.x; id < tiles; id += gridDim.x) {
     const typename T::Place at = next;
     f32x16 acc[TM][TN];
     if constexpr (kKept) T::template logits_of<false>(a, at, wave, lane, acc);
-    else T::template run<2>(at.source, lds, acc);
+    else T::template run<4>(at.source, lds, acc);
     const int c0 = at.c0, rows_v = at.rows_v, rows_n = at.rows_n;
     const int64_t n0 = at.n0;
     const int first = a.piece_first + c0 + wm * 32 * TM;
@@ -597,7 +590,7 @@ __global__ __launch_bounds__(64 * WGM * WGN) void class_grad_kernel(ClassArgs a)
       __syncthreads();  // every wavefront is done with the ring
       if (id + gridDim.x < tiles) {
         next = T::place(a, id + gridDim.x, tiles, count, a.piece_first, a.piece_classes);
-        T::template fill<0, 2>(next.source, lds);
+        T::template fill<0, 4>(next.source, lds);
       }
       add_bias<TM, TN>(a.bias, first, a.V, lane, acc);
     }
@@ -628,7 +621,7 @@ __global__ __launch_bounds__(64 * WGM * WGN) void class_grad_kernel(ClassArgs a)
 #pragma unroll
           for (int e = 0; e < 16; ++e) acc[i][j][e] = 32 * i + 8 * (e >> 2) + (e & 3) < classes ? acc[i][j][e] : 0.f;
       }
-      T::template store_block<j>(a, at, wave, lane, acc, strip);
+      T::template store_block<j>(a, at, wave, lane, acc);
     });
     if (a.column_sums) {
       // sums over the tile's rows: over j in registers, over 32 lanes by halving, over wavefronts through LDS

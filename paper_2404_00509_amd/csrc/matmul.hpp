@@ -218,7 +218,7 @@ struct Tile {
     int first, count;
   };
 
-  // The tile's sums.  kAhead: slices of the ring that fill() has been called for already (0, 2 or 4); no
+  // The tile's sums.  kAhead: slices of the ring that fill() has been called for already (0 or 4); no
   // wavefront uses what the others' places hold any more.
   // kOnes: B is made in LDS: the ring's places 0 to 2 are A's, 3 and 4 hold B, zero but for 64 values that the first
   // wavefront moves from slice to slice.
@@ -347,7 +347,7 @@ struct Tile {
     } else {
       fill<kAhead, 5>(src, lds);
       // slice 0 has landed; of what was issued here the rest may be on its way
-      static_assert(kAhead == 0 || kAhead == 2 || kAhead == 4, "whole slices of both operands");
+      static_assert(kAhead == 0 || kAhead == 4, "none, or whole slices of both operands");
       constexpr int kRest = kAhead == 4 ? 1 : 3;
       if (nk > 2) __builtin_amdgcn_s_waitcnt(wait_vm(kRest * NL));
       else if (nk > 1) __builtin_amdgcn_s_waitcnt(wait_vm((kRest - 1) * NL));
