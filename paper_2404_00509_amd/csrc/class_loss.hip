@@ -1,7 +1,7 @@
 // Softmax cross entropy of a linear head over many classes (the finetuning recipe's loss, Sec. 3, Sec. 5.2, with
 // its label smoothing), with the gradients of tokens, weight and bias, and without ever
-// holding the logits: they are made on the matrix cores tile by tile, reduced, and made again where the gradient needs
-// them.
+// holding the logits of a large call: they are made on the matrix cores tile by tile and reduced; for the gradient
+// something of them is kept where there is room, and the rest made again.
 //
 //   l = x W^T + b;  loss_n = lse(l_n) - (1 - s) l_n,y - s mean(l_n);  loss = mean of loss_n
 //   g = (softmax(l) - (1 - s) onehot(y) - s / V) grad_scale / count
@@ -11,11 +11,12 @@
 //             their count, which the later kernels read from memory.  What such a row holds (NaN, infinities) touches
 //             nothing.  For the gradient also the largest magnitudes among tokens and weight
 //   stats     tiles of logits -> per row and tile the maximum, the sum of exponentials under it, the sum of logits
-//             (smoothing) and the label's logit
+//             (smoothing) and the label's logit.  For the gradient also, without a bias, the exponentials of the first
+//             piece of the classes, with one all logits of a small call (class_plan)
 //   rows      the tiles of a row joined -> maximum, 1 / sum, the row's loss.  Beside it, for the gradient, tokens and
 //             weight as fp16
-//   grad      tiles of logits again -> g as fp16 [rows, classes of the piece], sums of its columns in fp32; one
-//             workgroup joins the loss (without gradient: a launch of its own)
+//   grad      what is kept, or tiles of logits again -> g as fp16 [rows, classes of the piece], sums of its columns in
+//             fp32; one workgroup joins the loss (without gradient: a launch of its own)
 //   products  g W (g along k, W across k) and g^T x (both across k) in one launch; few tiles: k is split
 //   finish    grad_bias, and the parts of a split joined, scaled, rounded once to bf16
 //
@@ -29,14 +30,16 @@
 // the loss: double precision.  g, an operand of two products, is fp16 and not bf16: |g| <= 1, so that as 2^15 g it
 // loses at most 2^-11 of a value down to 2^-29, an eighth of what bf16 would, and less than the bf16 outputs
 // do by their own rounding (with bf16 gradients were up to 1.5 times as far from the exact ones as results that are
-// rounded once, now within 1 %).  The other operand has to be fp16 too: scaled by the power of two that puts its
+// rounded once, now within 1 %).  Kept exponentials are 2^15 exp as fp16 likewise, under the maximum of their group of
+// classes; the label's g is made from its logit, so that nothing cancels.  A bias, whose gradient is a sum of g in single
+// precision, rules them out.  The other operand has to be fp16 too: scaled by the power of two that puts its
 // largest value just under 2^15, a bf16 number down to 2^-32 of that is exact.
 //
-// 16,384 x 1024 over 32,003 classes, a tenth of the rows left out, 3.87 TFLOP with the logits made twice: 3.6 to 3.7 ms.
-// pack 26 us, stats 940 (1.03 PFLOP/s), rows 48, and twice grad 510 and products 870 (1.13 PFLOP/s).  What bounds it is
-// the main loop (matmul.hpp), and beside it in stats and grad the exponentials: a tile of 256 x 256 with 16 slices
-// takes 33 us, 26 of them in the loop.  Small calls are bound by their launches: 64 x 192 over 1000 classes 28 us
-// for six, 4.5 us each.
+// 16,384 x 1024 over 32,003 classes, a tenth of the rows left out, 2.90 TFLOP: 3.1 ms (3.6 to 3.7 with the logits made
+// again).  pack 28 us, stats 1050 (0.92 PFLOP/s; 915 if nothing is kept), rows 58, grad 362 (1.9 GB, 5.2 TB/s), products 1630
+// (1.19 PFLOP/s).  What bounds it is the main loop (matmul.hpp), and beside it in stats the exponentials: a tile of
+// 256 x 256 with 16 slices takes 33 us, 26 of them in the loop, and storing exponentials 5 more.  Small calls are bound by
+// their launches: 64 x 192 over 1000 classes 28 us for six, 4.5 us each.
 #include "mae_device.hpp"
 #include "mae_kernels.hpp"
 #include "matmul.hpp"
@@ -905,9 +908,11 @@ static int products_side(int64_t M, int D, int V) {
   return M <= 256 || tiles(256) < 256 ? 128 : 256;
 }
 
-// What stats keeps for the gradient, so that the logits need not be made again: all logits in fp32 where they fit the
-// caches (64 MiB); else, if there is no gradient of a bias, which is to have single precision, the exponentials of the first
-// piece in the place of its g.
+// What stats keeps for the gradient, so that the logits need not be made again.  Without a bias: exponentials of the first
+// piece, as fp16 in the place of its g.  With one, whose gradient is to have single precision: the logits in fp32 if they fit
+// the caches with room to spare, 64 MiB.  us of whole calls with the logits made again / in fp32 / exponentials: 768 values, 1000
+// classes, 4096 rows 72.2 / 67.1 / 64.8, 16384 179 / 175 / 163, 32768 320 / 328 / 284; 512 x 768 over 32,003 182 / 172 / 159,
+// 16384 x 1024 over 32,003 4070 / - / 3390.
 constexpr int64_t kMostLogits = int64_t(1) << 24;
 
 ClassPlan class_plan(int64_t M, int D, int V, bool bias, bool smooth, bool grad) {
@@ -941,7 +946,7 @@ ClassPlan class_plan(int64_t M, int D, int V, bool bias, bool smooth, bool grad)
     if (p.piece > V) p.piece = V;
     p.piece_ld = (int)ceil_div(p.piece, 64) * 64;
     const int64_t padded = ceil_div(M, p.side) * ceil_div(V, p.side) * p.side * p.side;
-    p.keep = padded <= kMostLogits ? kKeepLogits : bias ? kKeepNone : kKeepExp;
+    p.keep = !bias ? kKeepExp : padded <= kMostLogits ? kKeepLogits : kKeepNone;
     p.top_ld = (int)ceil_div(p.piece, p.side) * 2;
     p.logits = take(p.keep == kKeepLogits ? (size_t)padded * 4 : 0);
     p.tops = take(p.keep == kKeepExp ? m * p.top_ld * 4 : 0);

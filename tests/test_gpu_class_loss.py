@@ -64,8 +64,8 @@ def test_sizes(M, D, V):
         _check(x, y, w, b, smoothing, what=f"M{M} D{D} V{V} bias {bias}")
 
 
-# logits kept in fp32 for the gradient up to 64 MiB, exponentials in fp16 beyond that without a bias, nothing with one; tiles
-# of all sides; the last group of classes whole, ragged and of one class
+# without a bias exponentials are kept for the gradient, with one the logits up to 64 MiB and nothing beyond; tiles of all
+# sides; the last group of classes whole, ragged and of one class
 @pytest.mark.parametrize("M,D,V", [(2048, 64, 8192), (2048, 64, 8193), (16390, 40, 1024), (17000, 8, 1000), (17, 24, 1 << 20),
                                    (200, 72, 90_001), (60, 16, 300_000)])
 def test_what_is_kept_for_the_gradient(M, D, V):
