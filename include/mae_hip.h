@@ -22,7 +22,7 @@
  *   mae_dropout           dropout and drop path from the keyed draws, no mask stored
  *   mae_layer_norm        layer norm of token rows (mae_layer_norm_grad: its backward pass)
  *   mae_class_loss        softmax cross entropy of a linear head over many classes, with label
- *                         smoothing, without keeping the logits
+ *                         smoothing, without keeping the logits of a large call
  * mae_prep_batch also takes JPEG files and decodes only the region each crop needs ("crop
  * decode", Sec. 4.1; mae_jpeg_index prepares files once for it) and applies the finetuning
  * augmentation (Sec. 4.4); mae_normpix_loss_from_images is the loss without a stored target;
@@ -448,8 +448,8 @@ size_t mae_layer_norm_workspace_bytes(const mae_norm_desc* d);
  * Rows with any other label (-1, say) are left out: their row_loss and grad_tokens are 0, and nothing that
  * such a row of `tokens` holds is used.  With no row left, loss and gradients are 0.  The logits of a large call
  * are never stored: they are made tile by tile, and the gradient goes through the classes in pieces of at most
- * 1 GiB of g; for the first one without a bias exponentials are kept, with a bias logits up to 64 MiB, the others'
- * are made again.  Operands are bf16, logits, maxima and sums single precision, the sum of row_loss double; before the
+ * 1 GiB of g or 1024 classes; for the first one without a bias exponentials are kept, with a bias logits up to
+ * 64 MiB, the others' are made again.  Operands are bf16, logits, maxima and sums single precision, the sum of row_loss double; before the
  * factor grad_scale / n, g is rounded to fp16 (of 2^15 g) as an operand of the two products, whose other operand
  * then is an fp16 copy scaled by a power of two: exact for values down to 2^-32 of the tensor's largest.
  * Exponentials that are kept are rounded to fp16 in the same way (not the label's).  grad_bias is summed before
