@@ -332,3 +332,34 @@ def test_side_stream_replays_of_a_graph_and_new_labels():
         torch.cuda.synchronize()
         for name, t in out.items():
             assert torch.equal(t, want[k % 2][name]), (k, name)
+
+
+@pytest.mark.parametrize("M,D,V", [(37, 64, 1003), (600, 192, 1000), (2060, 72, 4100)])
+def test_without_a_bias_the_same_bits_in_replays_of_a_graph_and_by_itself(M, D, V):
+    x, y, w, _ = _inputs(19, M, D, V, False, 0.2)
+    y2 = torch.where(torch.rand(M, device="cuda") < 0.5, torch.full_like(y, V), y.flip(0))
+    want = [_run(x, t, w, None, 0.1) for t in (y, y2)]
+    none = _run(x, y, w, None, 0.1, want=())
+    assert all(torch.equal(none[k], want[0][k]) for k in none)
+    for k in ("grad_tokens", "grad_weight"):
+        assert torch.equal(_run(x, y, w, None, 0.1, want=(k,))[k], want[0][k])
+    labels = y.clone()
+    desc = mae.make_class_desc(x, labels, w, smoothing=0.1)
+    n = mae.mae_class_loss_workspace_bytes(desc, True)
+    ws = torch.full((n + 4096,), 0x3C, dtype=torch.uint8, device="cuda")
+    out = {k: torch.empty_like(v) for k, v in want[0].items()}
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        mae.mae_class_loss(desc, out["loss"], out["row_loss"], out["grad_tokens"], out["grad_weight"], None, ws[:n],
+                           stream=torch.cuda.current_stream())
+    for k in range(4):
+        for t in out.values():
+            t.fill_(float("nan"))
+        ws[:n].fill_((0xFF, 0x00)[k // 2])
+        labels.copy_((y, y2)[k % 2])
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for name, t in out.items():
+            assert torch.equal(t, want[k % 2][name]), (k, name)
+        assert bool((ws[n:] == 0x3C).all())
