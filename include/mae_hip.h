@@ -446,14 +446,15 @@ size_t mae_layer_norm_workspace_bytes(const mae_norm_desc* d);
  *   g = (softmax(l) - (1 - s) onehot(label) - s / V) * grad_scale / n
  *   grad_tokens = g weight,  grad_weight = g^T tokens,  grad_bias = sum over rows of g
  * Rows with any other label (-1, say) are left out: their row_loss and grad_tokens are 0, and nothing that
- * such a row of `tokens` holds is used.  With no row left, loss and gradients are 0.  The logits of a large call
- * are never stored: they are made tile by tile, and the gradient goes through the classes in pieces of at most
- * 1 GiB of g or 1024 classes; for the first one without a bias exponentials are kept, with a bias logits up to
- * 64 MiB, the others' are made again.  Operands are bf16, logits, maxima and sums single precision, the sum of row_loss double; before the
- * factor grad_scale / n, g is rounded to fp16 (of 2^15 g) as an operand of the two products, whose other operand
- * then is an fp16 copy scaled by a power of two: exact for values down to 2^-32 of the tensor's largest.
- * Exponentials that are kept are rounded to fp16 in the same way (not the label's).  grad_bias is summed before
- * any such rounding.  A class whose bias is -infinity or the lowest float has probability 0.
+ * such a row of `tokens` holds is used. With no row left, loss and gradients are 0. The logits of a large
+ * call are never stored: they are made tile by tile, and the gradient goes through the classes in pieces of
+ * at most 1 GiB of g or 1024 classes; for the first one exponentials are kept without bias and smoothing,
+ * else logits up to 64 MiB; the others' are made again. Operands are bf16, logits, maxima and sums single
+ * precision, the sum of row_loss double; before the factor grad_scale / n, g is rounded to fp16 (of 2^15 g)
+ * as an operand of the two products, whose other operand then is an fp16 copy scaled by a power of two: exact
+ * for values down to 2^-32 of the tensor's largest. Exponentials that are kept are rounded to fp16 in the
+ * same way (not the label's). grad_bias is summed before any such rounding. A class whose bias is -infinity
+ * or the lowest float has probability 0.
  *
  * Limits: 1 <= M <= 2^24, 8 <= D <= 8192 with D % 8 == 0, 1 <= V <= 2^20, M * V <= 2^38.
  * tokens, weight, grad_tokens and grad_weight are 16-byte aligned.  Outputs do not overlap inputs.

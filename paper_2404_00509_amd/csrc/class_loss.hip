@@ -11,8 +11,8 @@
 //             their count, which the later kernels read from memory.  What such a row holds (NaN, infinities) touches
 //             nothing.  For the gradient also the largest magnitudes among tokens and weight
 //   stats     tiles of logits -> per row and tile the maximum, the sum of exponentials under it, the sum of logits
-//             (smoothing) and the label's logit.  For the gradient also, without a bias, the exponentials of the first
-//             piece of the classes, with one all logits of a small call (class_plan)
+//             (smoothing) and the label's logit.  For the gradient also, without bias and smoothing, the exponentials of
+//             the first piece of the classes, else all logits of a small call (class_plan)
 //   rows      the tiles of a row joined -> maximum, 1 / sum, the row's loss.  Beside it, for the gradient, tokens and
 //             weight as fp16
 //   grad      what is kept, or tiles of logits again -> g as fp16 [rows, classes of the piece], sums of its columns in
@@ -31,8 +31,8 @@
 // loses at most 2^-11 of a value down to 2^-29, an eighth of what bf16 would, and less than the bf16 outputs
 // do by their own rounding (with bf16 gradients were up to 1.5 times as far from the exact ones as results that are
 // rounded once, now within 1 %).  Kept exponentials are 2^15 exp as fp16 likewise, under the maximum of their group of
-// classes; the label's g is made from its logit, so that nothing cancels.  A bias, whose gradient is a sum of g in single
-// precision, rules them out.  The other operand has to be fp16 too: scaled by the power of two that puts its
+// classes; the label's g is made from its logit, and there is no smoothing, so that nothing cancels; nor a bias, whose
+// gradient is a sum of g in single precision.  The other operand has to be fp16 too: scaled by the power of two that puts its
 // largest value just under 2^15, a bf16 number down to 2^-32 of that is exact.
 //
 // 16,384 x 1024 over 32,003 classes, a tenth of the rows left out, 2.90 TFLOP: 3.1 ms (3.6 to 3.7 with the logits made
@@ -674,7 +674,7 @@ __global__ __launch_bounds__(64 * WGM * WGN) void class_grad_kernel(ClassArgs a)
   }
 }
 
-// ---- the same from the exponentials that stats has kept of the first piece ------------------------------------
+// ---- the same from the exponentials that stats has kept of the first piece (no smoothing) ---------------------
 // A workgroup: kKeptRows rows by 256 classes, eight classes of every eighth row per lane.
 constexpr int kKeptThreads = 256, kKeptColumns = 256, kKeptRows = 32;
 __global__ __launch_bounds__(kKeptThreads) void class_kept_kernel(ClassArgs a) {
@@ -686,7 +686,6 @@ __global__ __launch_bounds__(kKeptThreads) void class_kept_kernel(ClassArgs a) {
   const int64_t row0 = (int64_t)(blockIdx.x / chunks) * kKeptRows + (int)threadIdx.x / kLanesPerRow;
   const int c = (int)(blockIdx.x % chunks) * kKeptColumns + (int)(threadIdx.x % kLanesPerRow) * 8;
   if (row0 >= count || c >= a.piece_ld) return;
-  const float off = a.smoothing / (float)a.V * kGScale, label = (1.0f - a.smoothing) * kGScale;
   f16x8 e[kTurns];
 #pragma unroll
   for (int t = 0; t < kTurns; ++t)
@@ -700,9 +699,9 @@ __global__ __launch_bounds__(kKeptThreads) void class_kept_kernel(ClassArgs a) {
     const float scale = exp_neg(a.tops[row * a.top_ld + c / a.top_classes] - m) * inv;
     float v[8];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] = (float)e[t][k] * scale - off;
+    for (int k = 0; k < 8; ++k) v[k] = (float)e[t][k] * scale;
     if (y >= 0 && y < 8) {  // (the label's anew from its logit: what is left of 1 - exp / sum has no digits to lose)
-      const float own = exp_neg(a.label_logit[row] - m) * (inv * kGScale) - off - label;
+      const float own = exp_neg(a.label_logit[row] - m) * (inv * kGScale) - kGScale;
 #pragma unroll
       for (int k = 0; k < 8; ++k) v[k] = k == y ? own : v[k];
     }
@@ -908,11 +907,11 @@ static int products_side(int64_t M, int D, int V) {
   return M <= 256 || tiles(256) < 256 ? 128 : 256;
 }
 
-// What stats keeps for the gradient, so that the logits need not be made again.  Without a bias: exponentials of the first
-// piece, as fp16 in the place of its g.  With one, whose gradient is to have single precision: the logits in fp32 if they fit
-// the caches with room to spare, 64 MiB.  us of whole calls with the logits made again / in fp32 / exponentials: 768 values, 1000
-// classes, 4096 rows 72.2 / 67.1 / 64.8, 16384 179 / 175 / 163, 32768 320 / 328 / 284; 512 x 768 over 32,003 182 / 172 / 159,
-// 16384 x 1024 over 32,003 4070 / - / 3390.
+// What stats keeps for the gradient, so that the logits need not be made again.  Without bias and smoothing: exponentials of
+// the first piece, as fp16 in the place of its g.  Else, as a bias's gradient is to have single precision and p - s / V
+// may cancel: the logits in fp32 if they fit the caches with room to spare, 64 MiB.  us of whole calls with the logits made
+// again / in fp32 / exponentials: 768 values, 1000 classes, 4096 rows 72.2 / 67.1 / 64.8, 16384 179 / 175 / 163, 32768
+// 320 / 328 / 284; 512 x 768 over 32,003 182 / 172 / 159, 16384 x 1024 over 32,003 4070 / - / 3390.
 constexpr int64_t kMostLogits = int64_t(1) << 24;
 
 ClassPlan class_plan(int64_t M, int D, int V, bool bias, bool smooth, bool grad) {
@@ -946,7 +945,7 @@ ClassPlan class_plan(int64_t M, int D, int V, bool bias, bool smooth, bool grad)
     if (p.piece > V) p.piece = V;
     p.piece_ld = (int)ceil_div(p.piece, 64) * 64;
     const int64_t padded = ceil_div(M, p.side) * ceil_div(V, p.side) * p.side * p.side;
-    p.keep = !bias ? kKeepExp : padded <= kMostLogits ? kKeepLogits : kKeepNone;
+    p.keep = !bias && !smooth ? kKeepExp : padded <= kMostLogits ? kKeepLogits : kKeepNone;
     p.top_ld = (int)ceil_div(p.piece, p.side) * 2;
     p.logits = take(p.keep == kKeepLogits ? (size_t)padded * 4 : 0);
     p.tops = take(p.keep == kKeepExp ? m * p.top_ld * 4 : 0);

@@ -104,8 +104,8 @@ def dropout_keep(M, D, p, rows_per_draw, seed, batch_index, layer, row_base):
 # ---- softmax cross entropy of a linear head --------------------------------------------------------------
 def class_loss(tokens, labels, weight, bias, smoothing, grad_scale=1.0):
     """-> dict of results, dict of bounds.  The gradients' bounds are those of the stated method: logits summed in
-    fp32, 2^15 g rounded to fp16 for the products; without a bias g is made of
-    exponentials that were rounded so once before (those of the first piece of the classes), but for the label's."""
+    fp32, 2^15 g rounded to fp16 for the products; without bias and smoothing g is
+    made of exponentials that were rounded so once before (those of the first piece of the classes), but for the label's."""
     dev = tokens.device
     V, D = weight.shape
     M = tokens.shape[0]
@@ -150,7 +150,7 @@ def class_loss(tokens, labels, weight, bias, smoothing, grad_scale=1.0):
     e_g = p * (2 * worst[:, None] + rel[:, None] + 4 * U32 * (top - l).clamp(max=104.0) + 8 * U32) + 2 * U32 * (p + want)
     f = abs(grad_scale) / n
     e_round = 2.0 ** -11 * g.abs() + 2.0 ** -40  # half a step of fp16, and of its smallest numbers
-    if bias is None:
+    if bias is None and not smoothing:
         # an exponential under a maximum above it, e = 2^15 exp: half a step is 2^-11 of it, or 2^-40 of 1; then it is
         # multiplied by a factor of at most 1 that makes it p
         once = 2.0 ** -11 * p + 2.0 ** -40
