@@ -347,7 +347,8 @@ int mae_patch_embed(const mae_embed_desc* d, void* tokens, void* hip_stream);
  *   grad_weight[e, d] = sum_m g[m, e] visible[m, d]
  *   grad_bias[e]      = sum_m g[m, e]
  *   grad_pos[l, e]    = sum over the rows m with ids_keep[m] = l (clamped as above) of g[m, e]; rows
- *                       of patches that no token names become 0
+ *                       of patches that no token names become 0.  An infinity or a NaN in g reaches
+ *                       no other position than its row's
  * The products are exact in single precision; sums are kept in single precision or better, in a fixed
  * order (two calls give the same bits).  `weight`, `bias` and the values of `pos` are not read.
  *

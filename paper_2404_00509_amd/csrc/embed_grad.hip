@@ -23,7 +23,27 @@ using namespace mm;
 
 constexpr int kThreads = 256;
 
+// What a pass over rows that are not all finite takes in place of g: a count of +infinity and NaN, of -infinity and NaN, or
+// what is finite.
+enum Filter { kUp, kDown, kFinite };
+__device__ inline u32x4 filtered(u32x4 v, int filter) {
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    uint32_t out = 0;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const uint32_t x = v[w] >> (16 * h) & 0xFFFFu, size = x & 0x7FFFu;
+      const bool counts = size > 0x7F80u || x == (filter == kUp ? 0x7F80u : 0xFF80u);
+      out |= (filter == kFinite ? (size < 0x7F80u ? x : 0u) : counts ? 0x3F80u : 0u) << (16 * h);
+    }
+    v[w] = out;
+  }
+  return v;
+}
+
 // Part s of the sums: weight_acc[s][e][d], pos_acc[s][e][l].
+// In a product with zeros an infinity of one position is a NaN in all others (0 * inf).  That is how it is noticed: then the
+// tile is made again from the finite values, and infinities and NaN are added to the sums of their own positions.
 template <int TM, int TN, int WGM, int WGN>
 __global__ __launch_bounds__(64 * WGM * WGN) void embed_products_kernel(EmbedGradArgs a) {
   using T = Tile<TM, TN, WGM, WGN, false, false>;
@@ -41,6 +61,8 @@ __global__ __launch_bounds__(64 * WGM * WGN) void embed_products_kernel(EmbedGra
   const int64_t k0 = (int64_t)s0 * kSlice;
   const int depth = uniform(min(s1 * kSlice, K) - min(s0 * kSlice, K));
   const Operand A{a.g + k0 * a.ld + m0, a.ld, rows_m};
+  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+  const int wm = wave / WGN, wn = wave % WGN;
   f32x16 acc[TM][TN];
   float* out;
   int ld, rows_n;
@@ -58,9 +80,46 @@ __global__ __launch_bounds__(64 * WGM * WGN) void embed_products_kernel(EmbedGra
     T::template run<0, true>(T::source(A, A, depth), lds, acc, ones);
     ld = a.pos_columns;
     out = a.pos_acc + ((int64_t)part * a.E + m0) * ld + n0;
+    if (a.ids) {  // (without, every row has its 1 in the one column that is used)
+      bool nan = false;
+#pragma unroll
+      for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) nan |= acc[i][j][e] != acc[i][j][e];
+      uint32_t* seen = reinterpret_cast<uint32_t*>(lds);
+      __syncthreads();  // every wavefront is done with the ring
+      const bool any = __any(nan) != 0;
+      if (lane == 0) seen[wave] = any ? 1u : 0u;
+      __syncthreads();
+      uint32_t found = 0;
+#pragma unroll
+      for (int w = 0; w < WGM * WGN; ++w) found |= seen[w];
+      if (uniform((int)found) != 0) {
+        constexpr int kSums = TM * TN * 16, kWords = (kSums + 31) / 32;
+        uint32_t up[kWords] = {}, down[kWords] = {};  // a bit per sum of this lane
+        __syncthreads();
+#pragma unroll 1
+        for (int filter = kUp; filter <= kFinite; ++filter) {
+          T::run_filtered(A, depth, lds, acc, ones, [&](u32x4 v) { return filtered(v, filter); });
+#pragma unroll
+          for (int n = 0; n < kSums; ++n) {
+            const uint32_t bit = acc[n / 16 / TN][n / 16 % TN][n % 16] > 0.f ? 1u << (n % 32) : 0u;
+            if (filter == kUp) up[n / 32] |= bit;
+            if (filter == kDown) down[n / 32] |= bit;
+          }
+        }
+#pragma unroll
+        for (int n = 0; n < kSums; ++n) {
+          float sum = acc[n / 16 / TN][n / 16 % TN][n % 16];
+          if (up[n / 32] >> (n % 32) & 1u) sum += __builtin_inff();
+          if (down[n / 32] >> (n % 32) & 1u) sum -= __builtin_inff();
+          acc[n / 16 / TN][n / 16 % TN][n % 16] = sum;
+        }
+      }
+    }
   }
-  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-  const int wm = wave / WGN, wn = wave % WGN;
 #pragma unroll
   for (int i = 0; i < TM; ++i)
 #pragma unroll

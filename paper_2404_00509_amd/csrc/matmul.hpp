@@ -415,6 +415,72 @@ struct Tile {
     multiply(1);
   }
 
+  // The product with the ones by values that pass through `filter` (eight bf16 at a time) on their way to LDS: K rows
+  // of A through registers, a slice at a time.  For what is rare, so of few registers and little code; no wavefront uses the
+  // ring any more.
+  template <class F>
+  __device__ static inline void run_filtered(const Operand& A, int K, u32x4* lds, f32x16 (&acc)[TM][TN], const Ones& ones,
+                                             F&& filter) {
+    static_assert(!kAlongA && !kAlongB && !kHalf, "bf16 ones, across k");
+    typedef u32x4 u32x4_a4 __attribute__((aligned(4)));
+    const int lane = threadIdx.x % kWave, wave = uniform((int)threadIdx.x / kWave);
+    const int wm = wave / WGN, wn = wave % WGN;
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+      for (int j = 0; j < TN; ++j)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
+    const uint32_t lds_base = (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) u32x4*)lds;
+    const int g = lane >> 4, i16 = lane & 15;
+#pragma unroll 1
+    for (int k0 = 0; k0 < K; k0 += kSlice) {
+#pragma unroll 1
+      for (int slot = threadIdx.x; slot < kSlots; slot += kThreads) {
+        int row, chunk;
+        slot_place<BM, false>(slot, &row, &chunk);
+        u32x4 v = u32x4{0u, 0u, 0u, 0u};
+        int c = -1;  // of this chunk's columns, the one whose 1 this row has
+        if (k0 + row < K) {
+          const int from = 8 * chunk < A.limit ? 8 * chunk : 0;
+          v = filter(*reinterpret_cast<const u32x4_a4*>(A.p + (int64_t)(k0 + row) * A.ld + from));
+          c = min(max(ones.ids[k0 + row], 0), ones.count - 1) - ones.first - 8 * chunk;
+        }
+        lds[slot] = v;
+        const uint32_t one = (c & 1) ? 0x3F800000u : 0x3F80u;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) v[w] = c >= 0 && (c >> 1) == w ? one : 0u;
+        lds[kSlots + slot] = v;
+      }
+      __syncthreads();
+#pragma unroll 1
+      for (uint32_t ks = 0; ks < kSlice / 16; ++ks) {
+        u32x4 fa[TM], fb[TN];
+        uint32_t at[TM];
+#pragma unroll
+        for (int t = 0; t < TM; ++t) at[t] = lds_base + across_at<BM>(wm * TM + t, g, i16);
+        unroll<2 * TM>([&](auto r) { read_part<BM, false, 0, decltype(r)::value>(at, ks * 32 * BM, fa); });
+#pragma unroll
+        for (int t = 0; t < TN; ++t) at[t] = lds_base + across_at<BN>(wn * TN + t, g, i16);
+        unroll<2 * TN>([&](auto r) { read_part<BN, false, 0, decltype(r)::value>(at, kPlaceBytes + ks * 32 * BN, fb); });
+        __builtin_amdgcn_sched_barrier(0);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll
+        for (int i = 0; i < TM; ++i) asm volatile("" : "+v"(fa[i]));
+#pragma unroll
+        for (int j = 0; j < TN; ++j) asm volatile("" : "+v"(fb[j]));
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+          for (int j = 0; j < TN; ++j)
+            acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, fa[i]),
+                                                                __builtin_bit_cast(bf16x8, fb[j]), acc[i][j], 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      __syncthreads();
+    }
+  }
+
  private:
   // where lane (g, i) of a 32-column block reads: row i / 4 of its group of four, columns 16 (g % 2) + 4 (i % 4)
   template <int R>
