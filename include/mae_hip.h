@@ -354,7 +354,9 @@ int mae_patch_embed(const mae_embed_desc* d, void* tokens, void* hip_stream);
  *
  * Limits: those of mae_patch_embed, out_dtype = MAE_BF16 (MAE_ERR_DTYPE otherwise), and with `pos`
  * L <= 8192 (the work of grad_pos grows with L).  grad_tokens and grad_weight are 16-byte aligned.  Outputs do
- * not overlap inputs.  Which of the three are asked for does not change their bits.
+ * not overlap inputs.  The bits of grad_weight and grad_pos do not depend on what else is asked for; grad_bias
+ * is the sum of grad_pos where that is asked for too (in double precision, rounded once), else a sum over the rows
+ * in single precision, so that its last places may differ between the two.
  *   grad_weight [E, D] float, grad_bias [E] float, grad_pos [L, E] float    each nullable, not all;
  *                                           grad_pos only with `pos` in the descriptor
  *   workspace   mae_patch_embed_grad_workspace_bytes(d) bytes, 256-byte aligned (0: invalid descriptor) */

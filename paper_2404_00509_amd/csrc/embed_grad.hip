@@ -5,9 +5,11 @@
 //
 // All three are one product of two matrices with few results and a long sum (768 x 768 over 200 k rows): g^T times the
 // rows of `visible`, and g^T times a matrix that is 1 at column ids_keep[m] of row m, which is made in LDS and never
-// exists in memory; grad_bias is the sum of grad_pos.  Both operands lie with the sum's index as their row number and are
-// multiplied as they lie (matmul.hpp, "across k").  The products are exact, sums fp32.  The sum's index is split over the
-// compute units; a second kernel adds the parts in a fixed order.
+// exists in memory; grad_bias is the sum of grad_pos, or without that a single column of ones (by positions always, so that
+// it has the same bits with and without grad_pos, weight and bias alone take 22 % longer at 21,312 rows, 588 -> 1024, 256
+// patches, 2 % at the headline batch, and several times as long with thousands of patches).  Both operands lie with the
+// sum's index as their row number and are multiplied as they lie (matmul.hpp, "across k").  The products are exact, sums
+// fp32.  The sum's index is split over the compute units; a second kernel adds the parts in a fixed order.
 //
 // (Sorting the rows by their index and adding up the rows of each took seven launches and 181 us beside 208 for the
 // weight, 200,704 rows, 768 -> 768, 196 patches; as columns of the product they cost a third more tiles.)

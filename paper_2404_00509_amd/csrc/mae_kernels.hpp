@@ -341,7 +341,8 @@ struct EmbedGradPlan {
   int side, parts;
   size_t padded, weight_acc, pos_acc, bytes;
 };
-// L: 1 without positional rows.  The plan does not depend on which of the gradients a call wants, nor do their bits.
+// L: 1 without positional rows.  The plan does not depend on which of the gradients a call wants, nor do the bits of
+// grad_weight and grad_pos; those of grad_bias are the same in all calls with grad_pos, and in all without.
 EmbedGradPlan embed_grad_plan(int64_t M, int D, int E, int L);
 struct EmbedGradArgs {
   int64_t M, K;

@@ -1,5 +1,5 @@
 """Gradients of the patch embedding where the interface promises more than sums: infinities and NaN stay in their
-position, and bits do not depend on which of the outputs a call asks for."""
+position, and which bits do not depend on the outputs that a call asks for."""
 import itertools
 
 import pytest
@@ -10,6 +10,7 @@ import paper_2404_00509_amd as mae
 pytestmark = pytest.mark.gpu
 
 BF16 = torch.bfloat16
+U32 = torch.finfo(torch.float32).eps / 2
 NAN, INF = float("nan"), float("inf")
 
 
@@ -19,7 +20,7 @@ def _whole(seed, M, D, E, L, most=3):
     return r(M, D), r(M, E), torch.randint(0, L, (M,), generator=g, device="cuda", dtype=torch.int32)
 
 
-def _run(visible, g, ids, L, want=(True, True, True), desc=None, ws=None):
+def _run(visible, g, ids, L, want=(True, True, True)):
     E, D = g.shape[-1], visible.shape[-1]
     w = torch.zeros(E, D, dtype=BF16, device="cuda")  # not read
     pos = None if ids is None else torch.zeros(L, E, device="cuda")
@@ -94,3 +95,53 @@ def test_a_whole_gradient_that_is_not_finite():
     half = torch.where((ids % 4 == 0)[:, None], torch.full_like(g, INF), g)
     for got, want, name in zip(_run(visible, half, ids, L)[1:], _plain(visible, half, ids, L)[1:], ("bias", "pos")):
         _same(got, want, name)
+
+
+@pytest.mark.parametrize("M,D,E,L", [(3000, 588, 384, 64), (3000, 588, 70, 64), (3001, 12, 36, 300), (500, 64, 64, 16),
+                                     (30000, 768, 768, 196), (2500, 100, 70, 1)])
+def test_bits_and_what_else_is_asked_for(M, D, E, L):
+    g = torch.Generator(device="cuda").manual_seed(M + E)
+    visible = torch.randn(M, D, generator=g, device="cuda").to(BF16)
+    grad = torch.randn(M, E, generator=g, device="cuda").to(BF16)
+    ids = torch.randint(0, L, (M,), generator=g, device="cuda", dtype=torch.int32)
+    whole = _run(visible, grad, ids, L)
+    alone = _run(visible, grad, ids, L, (False, True, False))[1]
+    for want in itertools.product((False, True), repeat=3):
+        if any(want):
+            weight, bias, pos = _run(visible, grad, ids, L, want)
+            assert weight is None or torch.equal(weight, whole[0]), want
+            assert pos is None or torch.equal(pos, whole[2]), want
+            # the bias by positions, or in one sum without them
+            assert bias is None or torch.equal(bias, whole[1] if want[2] else alone), want
+    double = whole[2].double()
+    exact, size = grad.double().sum(0), grad.double().abs().sum(0)
+    # (64 sums of L / 64 in 64 bits each: at most half a step of fp32, and one of its double)
+    assert bool(((whole[1].double() - double.sum(0)).abs() <= U32 * (1 + 1e-6) * double.abs().sum(0)).all())
+    for bias in (whole[1], alone):  # M roundings of fp32 sums, one of the result
+        assert bool(((bias.double() - exact).abs() <= (M + 1) * U32 * size).all())
+    none = _run(visible, grad, None, L, (True, True, False))  # an embedding without positional rows
+    for want in ((True, False, False), (False, True, False)):
+        for a, b in zip(_run(visible, grad, None, L, want), none):
+            assert a is None or torch.equal(a, b), want
+
+
+def test_weight_and_bias_in_replays_of_a_graph():
+    M, D, E, L = 2500, 768, 384, 196
+    visible, g, ids = _whole(4, M, D, E, L)
+    want = _run(visible, g, ids, L, (True, True, False))
+    weight, pos = torch.zeros(E, D, dtype=BF16, device="cuda"), torch.zeros(L, E, device="cuda")
+    desc = mae.make_embed_desc(visible, ids, weight, None, pos)
+    ws = torch.empty(mae.mae_patch_embed_grad_workspace_bytes(desc), dtype=torch.uint8, device="cuda")
+    out = [torch.empty_like(t) for t in want[:2]]
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        mae.mae_patch_embed_grad(desc, g, *out, None, ws, stream=torch.cuda.current_stream())
+    for k in range(3):
+        for t in out:
+            t.fill_(NAN)
+        ws.fill_(0xFF)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(out, want)), k
