@@ -56,6 +56,8 @@ typedef int32_t i32x4_a4 __attribute__((ext_vector_type(4), aligned(4)));
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kNegInf = -__builtin_inff();
 constexpr float kGScale = 32768.0f;  // of g as fp16
+// Of logits in their sum: of up to 2^20 classes that are ruled out by the lowest float as their bias, it stays a float.
+constexpr float kSumScale = 0x1p-20f;
 // What stats leaves of the first piece for its gradient
 enum Keep { kKeepNone, kKeepLogits, kKeepExp };
 
@@ -353,7 +355,8 @@ __global__ __launch_bounds__(64 * WGM * WGN) void class_stats_kernel(ClassArgs a
 #pragma unroll
         for (int i = 0; i < TM; ++i)
 #pragma unroll
-          for (int e = 0; e < 16; ++e) sl += 32 * i + 8 * (e >> 2) + (e & 3) < classes ? acc[i][j][e] : 0.f;
+          for (int e = 0; e < 16; ++e)
+            sl += 32 * i + 8 * (e >> 2) + (e & 3) < classes ? acc[i][j][e] * kSumScale : 0.f;
       }
       if (rows_v < T::BM) {
 #pragma unroll
@@ -456,7 +459,7 @@ __device__ inline float join_row(const ClassArgs& a, int64_t slot, int lane) {
     sl += __shfl_xor(sl, off, kWave);
   }
   float v = (top + logf(s)) - (1.0f - a.smoothing) * own;
-  if (a.logit_sums) v -= a.smoothing * (sl / (float)a.V);
+  if (a.logit_sums) v -= a.smoothing * (sl / ((float)a.V * kSumScale));
   if (lane == 0 && a.peaks) {
     a.row_max[slot] = top;
     a.row_inv[slot] = 1.0f / s;

@@ -1,0 +1,78 @@
+"""Softmax cross entropy of a linear head at the ends of its inputs' ranges: biases of the lowest float under label
+smoothing, operands and upstream derivatives far from 1, single values far above the rest.  Against the formulas in
+64 bits."""
+import pytest
+import torch
+
+import paper_2404_00509_amd as mae
+from train_reference import U16, U32, check, class_loss
+
+pytestmark = pytest.mark.gpu
+
+BF16 = torch.bfloat16
+LOWEST = torch.finfo(torch.float32).min
+
+
+def _inputs(seed, M, D, V, bias=True):
+    g = torch.Generator(device="cuda").manual_seed(seed * 1000003 + M * 1009 + D * 31 + V)
+    randn = lambda *s: torch.randn(*s, generator=g, device="cuda")  # noqa: E731
+    w = (randn(V, D) / D ** 0.5).to(BF16)
+    y = torch.randint(0, V, (M,), generator=g, device="cuda", dtype=torch.int32)
+    x = (randn(M, D) + 2 * w[y.long()].float()).to(BF16)
+    return x, y, w, randn(V) if bias else None
+
+
+def _run(x, y, w, b, smoothing=0.0, grad_scale=1.0, grad=True):
+    desc = mae.make_class_desc(x, y, w, b, smoothing=smoothing, grad_scale=grad_scale)
+    nan = lambda *s, dtype=torch.float32: torch.full(s, float("nan"), dtype=dtype, device="cuda")  # noqa: E731
+    out = {"loss": nan(1), "row_loss": nan(desc.M)}
+    if grad:
+        out.update(grad_tokens=nan(*x.shape, dtype=BF16), grad_weight=nan(*w.shape, dtype=BF16))
+        if b is not None:
+            out["grad_bias"] = nan(desc.V)
+    ws = torch.full((mae.mae_class_loss_workspace_bytes(desc, grad),), 0xFF, dtype=torch.uint8, device="cuda")
+    mae.mae_class_loss(desc, out["loss"], out["row_loss"], out.get("grad_tokens"), out.get("grad_weight"),
+                       out.get("grad_bias"), ws)
+    torch.cuda.synchronize()
+    return out
+
+
+# tiles of 64, 128 and 256 classes; whole tiles of classes that are ruled out, parts of tiles, all but the labels'
+@pytest.mark.parametrize("M,D,V,ruled_out", [(40, 64, 300, 2), (40, 64, 300, 200), (300, 32, 9000, 8000),
+                                             (4100, 64, 8200, 5000), (1, 8, 1 << 20, (1 << 20) - 1)])
+def test_smoothing_over_classes_with_the_lowest_float_as_their_bias(M, D, V, ruled_out):
+    smoothing, left = 0.1, V - ruled_out
+    x, y, w, b = _inputs(1, M, D, V)
+    y, b = y % left, b.clone()
+    b[left:] = LOWEST
+    # what such a class adds to the mean of the logits is finite, and so is the loss
+    z = x.double() @ w[:left].double().T.contiguous() + b[:left].double()
+    lse = torch.logsumexp(z, 1)
+    mean = (z.sum(1) + ruled_out * LOWEST) / V  # (its own products are far below the last place of the lowest float)
+    row = lse - (1 - smoothing) * z[torch.arange(M, device="cuda"), y.long()] - smoothing * mean
+    assert bool(torch.isfinite(row.float()).all())
+    bound = (V + 16) * U32 * smoothing * mean.abs() + 1e-3  # V roundings of the sum, some of the rest; a small logit's
+    for grad in (False, True):
+        out = _run(x, y, w, b, smoothing, grad=grad)
+        check(out["row_loss"], row, bound, "row_loss")
+        check(out["loss"], row.mean().reshape(1), bound.mean() + U32 * row.mean().abs(), "loss")
+    # gradients: as with a bias that is low enough for a probability of 0 (exp(-200) is no float)
+    low = b.clone()
+    low[left:] = -200.0
+    ref, bound = class_loss(x, y, w, low, smoothing)
+    for k in ("grad_tokens", "grad_weight", "grad_bias"):
+        check(out[k], ref[k], bound[k], k)
+
+
+def test_a_class_with_an_infinite_bias_under_smoothing():
+    # the mean of the logits, and the loss, is infinite; the gradient is not
+    x, y, w, b = _inputs(2, 70, 64, 500)
+    y, b = y % 400, b.clone()
+    b[400:] = -float("inf")
+    out = _run(x, y, w, b, 0.1)
+    assert bool((out["row_loss"] == float("inf")).all()) and bool((out["loss"] == float("inf")).all())
+    low = b.clone()
+    low[400:] = -200.0
+    ref, bound = class_loss(x, y, w, low, 0.1)
+    for k in ("grad_tokens", "grad_weight", "grad_bias"):
+        check(out[k], ref[k], bound[k], k)
