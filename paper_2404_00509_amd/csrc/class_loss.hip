@@ -118,16 +118,18 @@ __device__ inline double grad_factor(const ClassArgs& a) {
   const int n = *a.count;
   return n > 0 ? (double)a.grad_scale / (double)n : 0.0;
 }
-// A product's sum to a gradient, with the powers of two of its operands taken out: `rest` is the factor of the
-// operand beside g.  (That factor may be as far from 1 as floats go, so it is not multiplied into `factor`.)
+// A product's sum to a gradient: a factor in [0.5, 1), and the powers of two of grad_scale, of the number of rows and of the
+// operands, none of which need be a float by itself (an upstream derivative of 1e38, operands of 1e-30).
 struct Scale {
   float factor;
-  int rest;
-  __device__ inline float operator()(float v) const { return ldexpf(v * factor, rest); }
+  int exponent;
+  __device__ inline float operator()(float v) const { return ldexpf(v * factor, exponent); }
 };
 __device__ inline Scale product_scale(const ClassArgs& a, bool by_weight) {
   const int from = by_weight ? a.pack_blocks : 0, to = by_weight ? a.num_peaks : a.pack_blocks;
-  return Scale{(float)(grad_factor(a) / (double)kGScale), -half_exponent(peak_among(a.peaks, from, to))};
+  int e;
+  const double m = frexp(grad_factor(a) / (double)kGScale, &e);
+  return Scale{(float)m, e - half_exponent(peak_among(a.peaks, from, to))};
 }
 
 // ---- pack -----------------------------------------------------------------------------------------
@@ -848,8 +850,9 @@ __global__ __launch_bounds__(kFinishThreads) void class_finish_kernel(ClassArgs 
     part[r][col] = s;
     __syncthreads();
     if (r == 0 && c < a.piece_classes)
-      a.grad_bias[a.piece_first + c] = ((part[0][col] + part[1][col]) + (part[2][col] + part[3][col])) *
-                                       (float)(grad_factor(a) / (double)kGScale);
+      a.grad_bias[a.piece_first + c] =
+          (float)((double)((part[0][col] + part[1][col]) + (part[2][col] + part[3][col])) *
+                  (grad_factor(a) / (double)kGScale));
     return;
   }
   block -= for_bias;

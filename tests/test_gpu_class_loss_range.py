@@ -76,3 +76,22 @@ def test_a_class_with_an_infinite_bias_under_smoothing():
     ref, bound = class_loss(x, y, w, low, 0.1)
     for k in ("grad_tokens", "grad_weight", "grad_bias"):
         check(out[k], ref[k], bound[k], k)
+
+
+# the gradients are floats, though their factors are not all: an upstream derivative near the largest float, one far below the
+# smallest of full precision, both ways round with the operands
+@pytest.mark.parametrize("grad_scale,of_tokens,of_weight,wanted", [
+    (1e38, 1e-5, 1.0, ("grad_tokens", "grad_weight", "grad_bias")), (-3e38, 1.0, 1e-6, ("grad_tokens", "grad_weight", "grad_bias")),
+    (2e-39, 1e30, 1e-30, ("grad_weight",)), (3e-42, 1e-30, 1e30, ("grad_tokens",)), (1e-37, 1.0, 1.0, ("grad_bias",)),
+    (1e30, 1e-30, 1e30, ("grad_weight", "grad_bias")), (1e-44, 1e36, 1e-30, ("grad_weight",))])
+@pytest.mark.parametrize("M", [9, 700])
+def test_upstream_derivatives_of_any_size(grad_scale, of_tokens, of_weight, wanted, M):
+    x, y, w, b = _inputs(3, M, 64, 300)
+    x, w = (x.float() * of_tokens).to(BF16), (w.float() * of_weight).to(BF16)
+    assert bool(torch.isfinite(x).all()) and bool(torch.isfinite(w).all())
+    scale = float(torch.tensor(grad_scale, dtype=torch.float32))
+    out = _run(x, y, w, b, 0.1, scale)
+    ref, bound = class_loss(x, y, w, b, 0.1, scale)
+    for k in ("loss", "row_loss") + wanted:
+        assert float(ref[k].abs().max()) < 3.3e38
+        check(out[k], ref[k], bound[k], k)
