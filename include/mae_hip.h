@@ -453,11 +453,13 @@ size_t mae_layer_norm_workspace_bytes(const mae_norm_desc* d);
  * call are never stored: they are made tile by tile, and the gradient goes through the classes in pieces of
  * at most 1 GiB of g or 1024 classes; for the first one exponentials are kept without bias and smoothing,
  * else logits up to 64 MiB; the others' are made again. Operands are bf16, logits, maxima and sums single
- * precision, the sum of row_loss double; before the factor grad_scale / n, g is rounded to fp16 (of 2^15 g)
- * as an operand of the two products, whose other operand then is an fp16 copy scaled by a power of two: exact
- * for values down to 2^-32 of the tensor's largest. Exponentials that are kept are rounded to fp16 in the
- * same way (not the label's). grad_bias is summed before any such rounding. A class whose bias is -infinity
- * or the lowest float has probability 0.
+ * precision, the sum of row_loss double; before the factor grad_scale / n, g is rounded to fp16 (of 2^15 g; what
+ * is below 2^-40 becomes 0) as an operand of the two products, whose other operand then is an fp16 copy scaled by
+ * a power of two: exact for values down to 2^-31 of the tensor's largest. If any eight neighbours (16 bytes of a
+ * row) that are not all zero have exponents more than 24 below that of the tensor's largest finite value, g is
+ * rounded to bf16 for both products instead, and their other operands are the tensors themselves. Exponentials
+ * that are kept are rounded to fp16 as g is (not the label's). grad_bias is summed before any such rounding. A
+ * class whose bias is -infinity or the lowest float has probability 0.
  *
  * Limits: 1 <= M <= 2^24, 8 <= D <= 8192 with D % 8 == 0, 1 <= V <= 2^20, M * V <= 2^38.
  * tokens, weight, grad_tokens and grad_weight are 16-byte aligned.  Outputs do not overlap inputs.

@@ -209,7 +209,8 @@ int mae_class_loss(const mae_class_desc* d, float* loss, float* row_loss, void* 
     a.partials = at(p.partials, (double*)nullptr);
   }
   if (grad) {
-    a.peaks = at(p.peaks, (int32_t*)nullptr);
+    a.ranges = at(p.ranges, (uint32_t*)nullptr);
+    a.wide = at(p.wide, (int32_t*)nullptr);
     a.row_max = at(p.row_max, (float*)nullptr);
     a.row_inv = at(p.row_inv, (float*)nullptr);
     a.half_tokens = at(p.half_tokens, (uint16_t*)nullptr);

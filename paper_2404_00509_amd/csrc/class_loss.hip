@@ -32,8 +32,11 @@
 // do by their own rounding (with bf16 gradients were up to 1.5 times as far from the exact ones as results that are
 // rounded once, now within 1 %).  Kept exponentials are 2^15 exp as fp16 likewise, under the maximum of their group of
 // classes; the label's g is made from its logit, and there is no smoothing, so that nothing cancels; nor a bias, whose
-// gradient is a sum of g in single precision.  The other operand has to be fp16 too: scaled by the power of two that puts its
-// largest value just under 2^15, a bf16 number down to 2^-32 of that is exact.
+// gradient is a sum of g in single precision.  What is below 2^-40 of g becomes 0.  The other operand has to be fp16 too: scaled
+// by the power of two that puts its largest value just under 2^15, a bf16 number down to 2^-31 of the largest is exact (to the
+// smallest there is, where the largest is below 2^-112).  Where values lie further apart than that (too_wide; one token of
+// 1e15 among tokens around 1, say), both products are of bf16 instead, with g rounded to it: found out on the device, at a
+// percent of a small call's time (4096 x 768 over 1000 classes 69.2 -> 70.0 us), nothing of a large one's.
 //
 // 16,384 x 1024 over 32,003 classes, a tenth of the rows left out, 2.90 TFLOP: 3.1 ms (3.6 to 3.7 with the logits made
 // again).  pack 28 us, stats 1050 (0.92 PFLOP/s; 915 if nothing is kept), rows 58, grad 362 (1.9 GB, 5.2 TB/s), products 1630
@@ -55,7 +58,8 @@ typedef int32_t i32x4_a4 __attribute__((ext_vector_type(4), aligned(4)));
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kNegInf = -__builtin_inff();
-constexpr float kGScale = 32768.0f;  // of g as fp16
+constexpr int kGExponent = 15;
+constexpr float kGScale = 1 << kGExponent;  // of g as fp16
 // Of logits in their sum: of up to 2^20 classes that are ruled out by the lowest float as their bias, it stays a float.
 constexpr float kSumScale = 0x1p-20f;
 // What stats leaves of the first piece for its gradient
@@ -70,43 +74,56 @@ __device__ inline int row_count(const ClassArgs& a) { return a.count ? uniform(*
 // ---- powers of two that bring the operands into the range of fp16 ---------------------------------------
 constexpr int kPackThreads = 256;
 
-// The larger of `peak` and the finite magnitudes among eight bf16 values, as bits.
-__device__ inline int32_t peak_of(int32_t peak, u32x4 v) {
+// Of finite magnitudes as bf16 bits: in the low half the largest; in the high half the smallest that the largest of any eight
+// neighbours is, where these are not all zero, counted down from infinity, so that both halves are maxima (of nothing: 0).
+__device__ inline uint32_t both(uint32_t a, uint32_t b) {
+  typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a), __builtin_bit_cast(u16x2, b)));
+}
+__device__ inline uint32_t range_of(u32x4 v) {
+  uint32_t peak = 0;
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
-    const int32_t lo = v[k] & 0x7FFF, hi = (v[k] >> 16) & 0x7FFF;
-    if (lo < 0x7F80) peak = max(peak, lo);
-    if (hi < 0x7F80) peak = max(peak, hi);
+    const uint32_t lo = v[k] & 0x7FFFu, hi = (v[k] >> 16) & 0x7FFFu;
+    if (lo < 0x7F80u) peak = max(peak, lo);
+    if (hi < 0x7F80u) peak = max(peak, hi);
   }
-  return peak;
+  return peak > 0 ? (0x7F80u - peak) << 16 | peak : 0u;
 }
-// The workgroup's largest to memory.
-__device__ inline void leave_peak(int32_t peak, int32_t* slots, int32_t* out) {
+__device__ inline int32_t most_of(uint32_t range) { return (int32_t)(range & 0xFFFFu); }
+__device__ inline int32_t least_of(uint32_t range) { return 0x7F80 - (int32_t)(range >> 16); }
+__device__ inline uint32_t over_lanes(uint32_t range) {
 #pragma unroll
-  for (int off = kWave / 2; off > 0; off >>= 1) peak = max(peak, __shfl_xor(peak, off, kWave));
+  for (int off = kWave / 2; off > 0; off >>= 1) range = both(range, (uint32_t)__shfl_xor((int)range, off, kWave));
+  return range;
+}
+// The workgroup's to memory.
+__device__ inline void leave_range(uint32_t range, uint32_t* slots, uint32_t* out) {
+  range = over_lanes(range);
   __syncthreads();
-  if (threadIdx.x % kWave == 0) slots[threadIdx.x / kWave] = peak;
+  if (threadIdx.x % kWave == 0) slots[threadIdx.x / kWave] = range;
   __syncthreads();
   if (threadIdx.x == 0) {
-    for (int w = 1; w < kPackThreads / kWave; ++w) peak = max(peak, slots[w]);
-    *out = peak;
+    for (int w = 1; w < kPackThreads / kWave; ++w) range = both(range, slots[w]);
+    *out = range;
   }
 }
+// Of the workgroups [from, to), by all lanes of a wavefront
+__device__ inline uint32_t range_among(const uint32_t* ranges, int from, int to) {
+  uint32_t range = 0;
+  for (int i = from + (int)(threadIdx.x % kWave); i < to; i += kWave) range = both(range, ranges[i]);
+  return over_lanes(range);
+}
+// Whether an operand goes beyond what an fp16 copy holds.  With the largest value just under 2^15, eight neighbours of which
+// the largest is 2^-25 of that are at most 2^-15 of it off (half a step of fp16's smallest numbers), a sixteenth of what g
+// loses by its rounding; what is smaller still would lose more, and in the end everything.
+__device__ inline bool too_wide(uint32_t range) { return (most_of(range) >> 7) - (least_of(range) >> 7) > 24; }
 // The factor that brings values of which `peak` is the largest under 2^15, as an exponent of two: fp16 holds
 // 2^15 times what is under 2.  At most 2^126 and at least 2^-113, so that it is a float and so is its inverse.
 __device__ inline int half_exponent(int32_t peak) {
   const int e = (peak >> 7) - 127;  // 2^e <= the largest value < 2^(e + 1)
   return min(14 - e, 126);
 }
-// Largest of the peaks [from, to), by all lanes of a wavefront
-__device__ inline int32_t peak_among(const int32_t* peaks, int from, int to) {
-  int32_t p = 0;
-  for (int i = from + (int)(threadIdx.x % kWave); i < to; i += kWave) p = max(p, peaks[i]);
-#pragma unroll
-  for (int off = kWave / 2; off > 0; off >>= 1) p = max(p, __shfl_xor(p, off, kWave));
-  return p;
-}
-
 __device__ inline uint32_t half_pair(float lo, float hi) {
   typedef float in2 __attribute__((ext_vector_type(2)));
   typedef _Float16 out2 __attribute__((ext_vector_type(2)));
@@ -118,6 +135,9 @@ __device__ inline double grad_factor(const ClassArgs& a) {
   const int n = *a.count;
   return n > 0 ? (double)a.grad_scale / (double)n : 0.0;
 }
+// What g is multiplied by if it is bf16: at most 1 / rows, so that sums over rows stay floats wherever the operand's values are.
+__device__ inline int wide_exponent(const ClassArgs& a) { return *a.count > 1 ? __clz(*a.count - 1) - 32 : 0; }
+
 // A product's sum to a gradient: a factor in [0.5, 1), and the powers of two of grad_scale, of the number of rows and of the
 // operands, none of which need be a float by itself (an upstream derivative of 1e38, operands of 1e-30).
 struct Scale {
@@ -126,31 +146,33 @@ struct Scale {
   __device__ inline float operator()(float v) const { return ldexpf(v * factor, exponent); }
 };
 __device__ inline Scale product_scale(const ClassArgs& a, bool by_weight) {
-  const int from = by_weight ? a.pack_blocks : 0, to = by_weight ? a.num_peaks : a.pack_blocks;
+  const int from = by_weight ? a.pack_blocks : 0, to = by_weight ? a.num_ranges : a.pack_blocks;
+  const int of_half = kGExponent + half_exponent(most_of(range_among(a.ranges, from, to)));
   int e;
-  const double m = frexp(grad_factor(a) / (double)kGScale, &e);
-  return Scale{(float)m, e - half_exponent(peak_among(a.peaks, from, to))};
+  const double m = frexp(grad_factor(a), &e);
+  return Scale{(float)m, e - (*a.wide ? wide_exponent(a) : of_half)};
 }
 
 // ---- pack -----------------------------------------------------------------------------------------
-// Workgroups from pack_blocks on look for the largest magnitude of the weight.
+// Workgroups from pack_blocks on look for the range of the weight's magnitudes.
 __global__ __launch_bounds__(kPackThreads) void class_pack_kernel(ClassArgs a) {
   __shared__ int32_t wave_sum[kPackThreads / kWave];
+  __shared__ uint32_t wave_range[kPackThreads / kWave];
   __shared__ int32_t map[kPackThreads];
   const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
-  int32_t peak = 0;
+  uint32_t range = 0;
   if ((int)blockIdx.x >= a.pack_blocks) {
     const u32x4* w = reinterpret_cast<const u32x4*>(a.weight);
-    const int64_t n = (int64_t)a.V * a.D / 8, step = (int64_t)(a.num_peaks - a.pack_blocks) * kPackThreads;
+    const int64_t n = (int64_t)a.V * a.D / 8, step = (int64_t)(a.num_ranges - a.pack_blocks) * kPackThreads;
     constexpr int kBatch = 4;  // loads in flight
     for (int64_t i = (int64_t)((int)blockIdx.x - a.pack_blocks) * kPackThreads + tid; i < n; i += kBatch * step) {
       u32x4 v[kBatch];
 #pragma unroll
       for (int k = 0; k < kBatch; ++k) v[k] = i + k * step < n ? w[i + k * step] : u32x4{0u, 0u, 0u, 0u};
 #pragma unroll
-      for (int k = 0; k < kBatch; ++k) peak = peak_of(peak, v[k]);
+      for (int k = 0; k < kBatch; ++k) range = both(range, range_of(v[k]));
     }
-    leave_peak(peak, wave_sum, a.peaks + blockIdx.x);
+    leave_range(range, wave_range, a.ranges + blockIdx.x);
     return;
   }
   const int64_t row0 = (int64_t)blockIdx.x * a.pack_rows;
@@ -200,7 +222,7 @@ __global__ __launch_bounds__(kPackThreads) void class_pack_kernel(ClassArgs a) {
         if (i >= chunks) break;
         const int row = i / per_row, c = i - row * per_row, to = map[row];
         if (to >= 0) {
-          if (a.peaks) peak = peak_of(peak, v[k]);
+          if (a.ranges) range = both(range, range_of(v[k]));
           reinterpret_cast<u32x4*>(a.packed + (int64_t)to * a.D)[c] = v[k];
         } else if (a.grad_tokens) {
           reinterpret_cast<u32x4*>(static_cast<uint16_t*>(a.grad_tokens) + (base + row) * a.D)[c] = u32x4{0u, 0u, 0u, 0u};
@@ -209,7 +231,7 @@ __global__ __launch_bounds__(kPackThreads) void class_pack_kernel(ClassArgs a) {
     }
   }
   if (end == a.M && tid == 0) *a.count = at;
-  if (a.peaks) leave_peak(peak, wave_sum, a.peaks + blockIdx.x);
+  if (a.ranges) leave_range(range, wave_range, a.ranges + blockIdx.x);
 }
 
 // ---- tiles of logits --------------------------------------------------------------------------------
@@ -291,12 +313,13 @@ struct Logits : Tile<TM, TN, WGM, WGN, true, true> {
         }
   }
 
-  // Rows 32 j .. + 31 of a wavefront's values as fp16 to g.  A lane has every second group of four classes of its row: the
+  // Rows 32 j .. + 31 of a wavefront's values as fp16 to g (as bf16, times `down`: kWide).  A lane has every second group of four classes of its row: the
   // halves of the wavefront swap theirs, so that each has groups of eight, 16 bytes.  (Through strips of LDS, 256
   // bytes along a row at a time: 3 % of a call over 32,003 classes more.)
-  template <int j>
+  template <int j, bool kWide = false>
   __device__ static inline void store_block(const ClassArgs& a, const Place& at, int wave, int lane,
-                                            const f32x16 (&acc)[TM][TN]) {
+                                            const f32x16 (&acc)[TM][TN], float down = 1.f) {
+    const auto pair = [&](float lo, float hi) { return kWide ? pack_bf16x2(lo * down, hi * down) : half_pair(lo, hi); };
     const int wm = wave / WGN, wn = wave % WGN;
     const int row = wn * 32 * TN + j * 32 + (lane & 31), c = at.c0 + wm * 32 * TM + 8 * (lane >> 5);
     uint16_t* to = a.g + (at.n0 + row) * (int64_t)a.piece_ld + c;
@@ -308,8 +331,8 @@ struct Logits : Tile<TM, TN, WGM, WGN, true, true> {
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
           const auto swapped = __builtin_amdgcn_permlane32_swap(
-              half_pair(acc[i][j][4 * q + 2 * k], acc[i][j][4 * q + 2 * k + 1]),
-              half_pair(acc[i][j][4 * q + 4 + 2 * k], acc[i][j][4 * q + 5 + 2 * k]), false, false);
+              pair(acc[i][j][4 * q + 2 * k], acc[i][j][4 * q + 2 * k + 1]),
+              pair(acc[i][j][4 * q + 4 + 2 * k], acc[i][j][4 * q + 5 + 2 * k]), false, false);
           v[k] = swapped[0];
           v[2 + k] = swapped[1];
         }
@@ -462,7 +485,7 @@ __device__ inline float join_row(const ClassArgs& a, int64_t slot, int lane) {
   }
   float v = (top + logf(s)) - (1.0f - a.smoothing) * own;
   if (a.logit_sums) v -= a.smoothing * (sl / ((float)a.V * kSumScale));
-  if (lane == 0 && a.peaks) {
+  if (lane == 0 && a.ranges) {
     a.row_max[slot] = top;
     a.row_inv[slot] = 1.0f / s;
   }
@@ -470,12 +493,12 @@ __device__ inline float join_row(const ClassArgs& a, int64_t slot, int lane) {
 }
 
 constexpr int kRowThreads = 256, kRowWaves = kRowThreads / kWave;
-// Workgroups from row_blocks on make the fp16 copies, eight values per lane.
+// Workgroups from row_blocks on make the fp16 copies, eight values per lane, and find out whether they do.
 __global__ __launch_bounds__(kRowThreads) void class_rows_kernel(ClassArgs a) {
   if ((int)blockIdx.x >= a.row_blocks) {
+    const uint32_t of_t = range_among(a.ranges, 0, a.pack_blocks), of_w = range_among(a.ranges, a.pack_blocks, a.num_ranges);
     const int64_t of_tokens = (int64_t)*a.count * (a.D / 8), of_weight = (int64_t)a.V * (a.D / 8);
-    const float ft = ldexpf(1.0f, half_exponent(peak_among(a.peaks, 0, a.pack_blocks)));
-    const float fw = ldexpf(1.0f, half_exponent(peak_among(a.peaks, a.pack_blocks, a.num_peaks)));
+    const float ft = ldexpf(1.0f, half_exponent(most_of(of_t))), fw = ldexpf(1.0f, half_exponent(most_of(of_w)));
     const int64_t step = (int64_t)((int)gridDim.x - a.row_blocks) * kRowThreads;
     for (int64_t i = (int64_t)((int)blockIdx.x - a.row_blocks) * kRowThreads + threadIdx.x; i < of_tokens + of_weight;
          i += step) {
@@ -488,6 +511,8 @@ __global__ __launch_bounds__(kRowThreads) void class_rows_kernel(ClassArgs a) {
       for (int k = 0; k < 4; ++k) out[k] = half_pair(bf16_lo(v[k]) * f, bf16_hi(v[k]) * f);
       reinterpret_cast<u32x4*>(t ? a.half_tokens : a.half_weight)[at] = out;
     }
+    // (behind the loop: in front of it the compiler would not read the number of rows before it has stored this)
+    if ((int)blockIdx.x == a.row_blocks && threadIdx.x == 0) *a.wide = too_wide(of_t) || too_wide(of_w) ? 1 : 0;
     return;
   }
   __shared__ double sums[kRowWaves];
@@ -577,6 +602,8 @@ __global__ __launch_bounds__(64 * WGM * WGN) void class_grad_kernel(ClassArgs a)
   static_assert(kRoomBytes <= T::kPlaceBytes, "room in a place");
   __shared__ __attribute__((aligned(1024))) u32x4 lds[(kKept ? kRoomBytes : T::kLdsBytes) / 16];
   const int count = uniform(*a.count);
+  const bool wide = uniform(*a.wide) != 0;
+  const float down = ldexpf(1.0f / kGScale, wide_exponent(a));
   const uint32_t tiles = T::tiles(count, a.piece_classes);
   // (with the first piece: the loss, by a workgroup that has no more tiles than any other)
   if (a.piece_first == 0 && blockIdx.x == gridDim.x - 1) join_losses(a, reinterpret_cast<double*>(lds));
@@ -629,7 +656,8 @@ __global__ __launch_bounds__(64 * WGM * WGN) void class_grad_kernel(ClassArgs a)
 #pragma unroll
           for (int e = 0; e < 16; ++e) acc[i][j][e] = 32 * i + 8 * (e >> 2) + (e & 3) < classes ? acc[i][j][e] : 0.f;
       }
-      T::template store_block<j>(a, at, wave, lane, acc);
+      if (wide) T::template store_block<j, true>(a, at, wave, lane, acc, down);
+      else T::template store_block<j>(a, at, wave, lane, acc);
     });
     if (a.column_sums) {
       // sums over the tile's rows: over j in registers, over 32 lanes by halving, over wavefronts through LDS
@@ -687,6 +715,8 @@ __global__ __launch_bounds__(kKeptThreads) void class_kept_kernel(ClassArgs a) {
   __shared__ double sums[kRowWaves];
   if (blockIdx.x == gridDim.x - 1) join_losses(a, sums);
   const int count = uniform(*a.count);
+  const bool wide = uniform(*a.wide) != 0;
+  const float down = ldexpf(1.0f / kGScale, wide_exponent(a));
   const uint32_t chunks = (uint32_t)((a.piece_classes + kKeptColumns - 1) / kKeptColumns);
   const int64_t row0 = (int64_t)(blockIdx.x / chunks) * kKeptRows + (int)threadIdx.x / kLanesPerRow;
   const int c = (int)(blockIdx.x % chunks) * kKeptColumns + (int)(threadIdx.x % kLanesPerRow) * 8;
@@ -712,8 +742,10 @@ __global__ __launch_bounds__(kKeptThreads) void class_kept_kernel(ClassArgs a) {
     }
     u32x4 out;
 #pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = c + k < a.piece_classes ? v[k] : 0.f;
+#pragma unroll
     for (int k = 0; k < 4; ++k)
-      out[k] = half_pair(c + 2 * k < a.piece_classes ? v[2 * k] : 0.f, c + 2 * k + 1 < a.piece_classes ? v[2 * k + 1] : 0.f);
+      out[k] = wide ? pack_bf16x2(v[2 * k] * down, v[2 * k + 1] * down) : half_pair(v[2 * k], v[2 * k + 1]);
     *reinterpret_cast<u32x4*>(a.g + row * a.piece_ld + c) = out;
   }
 }
@@ -721,8 +753,9 @@ __global__ __launch_bounds__(kKeptThreads) void class_kept_kernel(ClassArgs a) {
 // ---- products ---------------------------------------------------------------------------------------
 // Part s of the sums over k of A(m, k) B[k][n], B with k as its row number; k is split into parts.
 struct Product {
-  const uint16_t* A;  // "along": A[m][k]; otherwise A[k][m]
-  const uint16_t* B;
+  const uint16_t* A;       // "along": A[m][k]; otherwise A[k][m]
+  const uint16_t* B;       // fp16 copy
+  const uint16_t* B_wide;  // bf16, if that would not do
   int64_t lda, ldb;   // values from row to row
   int M, N, K, parts;
   const int32_t* rows;    // nullable: only so many m (device memory)
@@ -734,9 +767,9 @@ struct Product {
   bool by_weight;         // B is the weight's copy (tokens' otherwise)
 };
 
-template <int TM, int TN, int WGM, int WGN, bool kAlongA>
+template <int TM, int TN, int WGM, int WGN, bool kAlongA, bool kWide>
 __device__ inline void product_tile(const ClassArgs& a, const Product& p, uint32_t block, uint32_t blocks, u32x4* lds) {
-  using T = Tile<TM, TN, WGM, WGN, kAlongA, false, true>;
+  using T = Tile<TM, TN, WGM, WGN, kAlongA, false, !kWide>;
   const int M = p.rows ? min(uniform(*p.rows), p.M) : p.M;
   const int K = p.depth ? min(uniform(*p.depth), p.K) : p.K;
   const uint32_t tiles_n = (uint32_t)((p.N + T::BN - 1) / T::BN);
@@ -753,7 +786,7 @@ __device__ inline void product_tile(const ClassArgs& a, const Product& p, uint32
   const int64_t k0 = (int64_t)s0 * kSlice;
   const int depth = uniform(min(s1 * kSlice, K) - min(s0 * kSlice, K));
   const Operand A{kAlongA ? p.A + m0 * p.lda + k0 : p.A + k0 * p.lda + m0, p.lda, rows_m};
-  const Operand B{p.B + k0 * p.ldb + n0, p.ldb, rows_n};
+  const Operand B{(kWide ? p.B_wide : p.B) + k0 * p.ldb + n0, p.ldb, rows_n};
   f32x16 acc[TM][TN];
   T::template run<0>(T::source(A, B, depth), lds, acc);
 
@@ -812,8 +845,15 @@ template <int TM, int TN, int WGM, int WGN>
 __global__ __launch_bounds__(64 * WGM * WGN) void class_products_kernel(ClassArgs a, Product tokens, Product weight,
                                                                         uint32_t of_tokens) {
   __shared__ __attribute__((aligned(1024))) u32x4 lds[Tile<TM, TN, WGM, WGN, true, false, true>::kLdsBytes / 16];
-  if (blockIdx.x < of_tokens) product_tile<TM, TN, WGM, WGN, true>(a, tokens, blockIdx.x, of_tokens, lds);
-  else product_tile<TM, TN, WGM, WGN, false>(a, weight, blockIdx.x - of_tokens, gridDim.x - of_tokens, lds);
+  const bool wide = uniform(*a.wide) != 0, first = blockIdx.x < of_tokens;
+  const uint32_t block = first ? blockIdx.x : blockIdx.x - of_tokens, blocks = first ? of_tokens : gridDim.x - of_tokens;
+  if (wide) {
+    if (first) product_tile<TM, TN, WGM, WGN, true, true>(a, tokens, block, blocks, lds);
+    else product_tile<TM, TN, WGM, WGN, false, true>(a, weight, block, blocks, lds);
+  } else {
+    if (first) product_tile<TM, TN, WGM, WGN, true, false>(a, tokens, block, blocks, lds);
+    else product_tile<TM, TN, WGM, WGN, false, false>(a, weight, block, blocks, lds);
+  }
 }
 
 // ---- finish -----------------------------------------------------------------------------------------
@@ -938,7 +978,8 @@ ClassPlan class_plan(int64_t M, int D, int V, bool bias, bool smooth, bool grad)
   p.logit_sums = take(smooth ? m * p.stat_tiles * 4 : 0);
   p.label_logit = take(m * 4);
   if (!p.few) {
-    p.count = take(sizeof(int32_t));
+    p.count = take(2 * sizeof(int32_t));
+    p.wide = p.count + sizeof(int32_t);  // (in one cache line: both are read where a kernel begins)
     p.label_of = take(m * 4);
     p.row_of = take(m * 4);
     p.packed = take(m * D * 2);
@@ -960,10 +1001,10 @@ ClassPlan class_plan(int64_t M, int D, int V, bool bias, bool smooth, bool grad)
     const bool many = ceil_div(p.piece, p.products_side) * ceil_div(D, p.products_side) >= 256;
     p.tokens_parts = product_parts(M, D, p.piece, p.products_side, many ? 128 : 256);
     p.weight_parts = product_parts(p.piece, D, M, p.products_side, 256);
-    p.num_weight_peaks = (int)(ceil_div((int64_t)V * D / 8, kPackThreads * 4) < 1024
-                                   ? ceil_div((int64_t)V * D / 8, kPackThreads * 4) : 1024);
-    p.num_peaks = (int)ceil_div(M, p.pack_rows) + p.num_weight_peaks;
-    p.peaks = take((size_t)p.num_peaks * 4);
+    const int64_t for_weight = ceil_div((int64_t)V * D / 8, kPackThreads * 4);
+    const int num_weight_ranges = (int)(for_weight < 1024 ? for_weight : 1024);
+    p.num_ranges = (int)ceil_div(M, p.pack_rows) + num_weight_ranges;
+    p.ranges = take((size_t)p.num_ranges * 4);
     p.row_max = take(m * 4);
     p.row_inv = take(m * 4);
     p.half_tokens = take(m * D * 2);
@@ -1028,11 +1069,11 @@ hipError_t launch_class_loss(ClassArgs a, const ClassPlan& p, hipStream_t stream
   a.pack_rows = p.pack_rows;
   a.stat_tiles = p.stat_tiles;
   a.pack_blocks = (int)ceil_div(a.M, p.pack_rows);
-  a.num_peaks = p.num_peaks;
+  a.num_ranges = p.num_ranges;
   a.row_blocks = p.row_blocks;
-  const bool grad = a.peaks != nullptr;
+  const bool grad = a.ranges != nullptr;
   if (!p.few)
-    hipLaunchKernelGGL(class_pack_kernel, dim3((uint32_t)(grad ? p.num_peaks : a.pack_blocks)), dim3(kPackThreads), 0,
+    hipLaunchKernelGGL(class_pack_kernel, dim3((uint32_t)(grad ? p.num_ranges : a.pack_blocks)), dim3(kPackThreads), 0,
                        stream, a);
   a.piece_first = 0;
   a.piece_classes = p.piece;
@@ -1071,12 +1112,14 @@ hipError_t launch_class_loss(ClassArgs a, const ClassPlan& p, hipStream_t stream
       // rows: packed rows; k: classes of the piece (g holds zeros up to a multiple of 8 behind them)
       tokens.A = a.g, tokens.lda = p.piece_ld;
       tokens.B = a.half_weight + (int64_t)first * a.D, tokens.ldb = a.D, tokens.by_weight = true;
+      tokens.B_wide = static_cast<const uint16_t*>(a.weight) + (int64_t)first * a.D;
       tokens.M = (int)a.M, tokens.N = a.D, tokens.K = a.piece_classes, tokens.rows = a.count;
       tokens.parts = p.tokens_parts, tokens.acc = a.tokens_acc, tokens.accumulate = first > 0;
       if (last) tokens.out = static_cast<uint16_t*>(a.grad_tokens), tokens.row_of = a.row_of;
     }
     if (a.grad_weight) {
       weight.A = a.g, weight.lda = p.piece_ld, weight.B = a.half_tokens, weight.ldb = a.D;
+      weight.B_wide = a.packed;
       weight.M = a.piece_classes, weight.N = a.D, weight.K = (int)a.M, weight.depth = a.count;
       weight.parts = p.weight_parts, weight.acc = a.weight_acc;
       weight.out = static_cast<uint16_t*>(a.grad_weight) + (int64_t)first * a.D;

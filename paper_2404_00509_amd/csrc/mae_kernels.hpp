@@ -287,10 +287,10 @@ struct ClassPlan {
   int piece, piece_ld;                // classes per piece of the gradient; row length of g
   int keep, top_ld;                   // what stats leaves for the gradient; row length of tops
   int products_side, tokens_parts, weight_parts;  // of the products for grad_tokens and grad_weight
-  int num_peaks, num_weight_peaks;    // workgroups of the first kernel; of them, those that look at the weight
+  int num_ranges;                     // workgroups of the first kernel that leave a range
   // places in the workspace
   size_t stats, logit_sums, label_logit, count, label_of, row_of, packed, partials;
-  size_t peaks, row_max, row_inv, half_tokens, half_weight, g, column_sums, tokens_acc, weight_acc, logits, tops;
+  size_t ranges, wide, row_max, row_inv, half_tokens, half_weight, g, column_sums, tokens_acc, weight_acc, logits, tops;
   size_t bytes;
 };
 ClassPlan class_plan(int64_t M, int D, int V, bool bias, bool smooth, bool grad);
@@ -316,7 +316,8 @@ struct ClassArgs {
   float* logit_sums;   // [slot][stat_tiles], null without smoothing
   float* label_logit;  // [slot]
   double* partials;    // [row_blocks] sums of losses
-  int32_t* peaks;      // [num_peaks] largest finite magnitudes as bf16 bits: tokens, then weight; null: no gradient
+  uint32_t* ranges;    // [num_ranges] of finite magnitudes: tokens, then weight; null: no gradient
+  int32_t* wide;       // 1: one of them is too wide for an fp16 copy, the products are of bf16
   float* row_max;      // [slot]
   float* row_inv;      // [slot] 1 / sum of exponentials under the maximum
   uint16_t* half_tokens;  // [slot][D] fp16, scaled by a power of two
@@ -328,7 +329,7 @@ struct ClassArgs {
   float* tokens_acc;      // [tokens_parts][M][D]
   float* weight_acc;      // [weight_parts][classes of the piece][D]
   // filled in by the launcher
-  int32_t pack_rows, stat_tiles, pack_blocks, num_peaks, row_blocks;
+  int32_t pack_rows, stat_tiles, pack_blocks, num_ranges, row_blocks;
   int32_t piece_first, piece_classes, piece_ld, grad_rows, tokens_parts, weight_parts;
   int32_t top_ld, top_classes;
 };

@@ -95,3 +95,102 @@ def test_upstream_derivatives_of_any_size(grad_scale, of_tokens, of_weight, want
     for k in ("loss", "row_loss") + wanted:
         assert float(ref[k].abs().max()) < 3.3e38
         check(out[k], ref[k], bound[k], k)
+
+
+def _check_bf16(x, y, w, b, smoothing, what):
+    """Against the formulas; with an operand whose range is too wide for fp16 g is rounded to bf16 for the products."""
+    out = _run(x, y, w, b, smoothing)
+    ref, bound = class_loss(x, y, w, b, smoothing)
+    ok = (y >= 0) & (y < w.shape[0])
+    xs, ys, ws = x[ok].double(), y[ok].long(), w.double()
+    z = xs @ ws.T.contiguous()
+    g = torch.softmax(z if b is None else z + b.double(), 1) - smoothing / w.shape[0]
+    g[torch.arange(len(ys), device="cuda"), ys] -= 1 - smoothing
+    once = U16 * g.abs() / len(ys)
+    bound["grad_tokens"][ok] += once @ ws.abs()
+    bound["grad_weight"] += once.T.contiguous() @ xs.abs()
+    for k, v in out.items():
+        check(v, ref[k], bound[k], f"{what} {k}")
+
+
+# exponentials kept, logits kept, nothing kept; tiles of 64, 128 and 256 of the logits and of the products
+CALLS = [(300, 64, 200, False), (300, 64, 200, True), (4100, 136, 8200, False), (4100, 136, 8200, True),
+         (4100, 1536, 8200, True), (40, 24, 1003, False)]
+
+
+@pytest.mark.parametrize("M,D,V,bias", CALLS)
+@pytest.mark.parametrize("size", [2.0 ** 40, 2.0 ** 90, 3e38])
+def test_one_token_value_far_above_the_rest(M, D, V, bias, size):
+    x, y, w, b = _inputs(4, M, D, V, bias)
+    w[:, 3] = (w[:, 3].float() * 0.25).to(BF16)
+    w[5, 3] = 1.0  # the row's one class
+    x[7, 3] = size
+    y[::9] = -1
+    y[7] = 11
+    _check_bf16(x, y, w, b, 0.1 if bias else 0.0, f"{size}")
+
+
+@pytest.mark.parametrize("M,D,V,bias", CALLS)
+@pytest.mark.parametrize("size", [2.0 ** 40, 3e38])
+def test_one_weight_far_above_the_rest(M, D, V, bias, size):
+    x, y, w, b = _inputs(5, M, D, V, bias)
+    x[:, 3] = 0.0
+    w[V // 2, 3] = size
+    _check_bf16(x, y, w, b, 0.1 if bias else 0.0, f"{size}")
+
+
+def test_values_far_above_the_rest_and_classes_in_pieces():
+    x, y, w, b = _inputs(6, 1 << 18, 8, 2100, False)
+    x[:, 3] = 0.0
+    w[5, 3] = 2.0 ** 70
+    _check_bf16(x, y, w, b, 0.0, "pieces")
+
+
+@pytest.mark.parametrize("rows", [1, 2, 3, 1000])
+def test_products_with_values_of_any_size_are_exact(rows):
+    # no weights: the probabilities are 1/2, g is -1/2 and 1/2, and the second class's gradient is the rows' mean / 2
+    small = 255.0 * 2.0 ** -38  # the last place of 8 bits 2^-38 below the largest value, a power of two
+    cases = [[0.0, 1.0, small, -small, 2.0 ** -31, 0.0, 3.0 * 2.0 ** -31, 1.0] + [small * 2] * 7 + [1.0],
+             [2.0 ** 100] + [0.0] * 7 + [1.5, -2.0 ** -7, 3.0] + [2.0 ** -40] * 5,
+             [3.0 * 2.0 ** 126, 1.0] + [2.0 ** -60] * 6 + [5.0 * 2.0 ** -90] * 8,
+             [2.0 ** -120, 2.0 ** -125, 2.0 ** -124, 0.0] * 2 + [3.0 * 2.0 ** -122] * 8]
+    for values in cases:
+        x = torch.tensor([values], dtype=torch.float64, device="cuda")
+        assert torch.equal(x.to(BF16).double(), x)
+        x = x.to(BF16).repeat(rows, 1)
+        y = torch.zeros(rows, dtype=torch.int32, device="cuda")
+        w = torch.zeros(2, 16, dtype=BF16, device="cuda")
+        for b in (None, torch.zeros(2, device="cuda")):
+            out = _run(x, y, w, b, 0.0)
+            want = x[0].double() / 2
+            # (sums of equal numbers: powers of two of rows are exact, 3 and 1000 are divided out again in fp32)
+            off = 0.0 if rows <= 2 else 3 * U32
+            got = out["grad_weight"].double()
+            assert bool(((got[1] - want).abs() <= off * want.abs()).all()), (rows, values, got[1], want)
+            assert torch.equal(got[0], -got[1])
+
+
+def test_replays_of_a_graph_whose_inputs_change_their_range():
+    M, D, V = 600, 192, 1000
+    x, y, w, b = _inputs(7, M, D, V)
+    far = x.clone()
+    far[::50, 5] = 2.0 ** 60
+    desc = mae.make_class_desc(x, y, w, b, smoothing=0.1)
+    want = [_run(t, y, w, b, 0.1) for t in (x, far)]
+    assert not torch.equal(want[0]["grad_weight"], want[1]["grad_weight"])
+    near, out = x.clone(), {k: torch.empty_like(v) for k, v in want[0].items()}
+    ws = torch.empty(mae.mae_class_loss_workspace_bytes(desc, True), dtype=torch.uint8, device="cuda")
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        mae.mae_class_loss(desc, *out.values(), ws, stream=torch.cuda.current_stream())
+    for k in range(4):
+        for t in out.values():
+            t.fill_(float("nan"))
+        ws.fill_((0xFF, 0x00)[k // 2])
+        x.copy_((near, far)[k % 2])
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for name, t in out.items():
+            assert torch.equal(t, want[k % 2][name]), (k, name)
