@@ -243,7 +243,10 @@ __global__ __launch_bounds__(threads<kLanes>()) void layer_norm_grad_kernel(Norm
       for (int v = 0; v < NV; ++v) {
         h[u][v] = (values(next_x[u][v]) - next_mean[u]) * rstd[u];
         g[u][v] = values(next_g[u][v]);
-        if (kParams) {  // (values that do not exist have a zero gradient)
+        // (values that do not exist have a zero gradient; mean and rstd may be so large that h is none that can meet it)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) h[u][v][j] = j < n[v] ? h[u][v][j] : 0.f;
+        if (kParams) {
           gw[v] += g[u][v] * h[u][v];
           gb[v] += g[u][v];
         }
