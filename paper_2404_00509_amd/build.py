@@ -7,6 +7,8 @@ import sys
 import tempfile
 from concurrent.futures import ThreadPoolExecutor
 
+from . import lds_reads
+
 _HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(_HERE, "csrc")
 SOURCES = ["api.hip", "api_train.hip", "mask_params.hip", "crop_patch.hip", "normpix_loss.hip",
@@ -33,17 +35,30 @@ def _run(cmd, verbose: bool) -> None:
         print(log, flush=True)
 
 
+def compile_source(source: str, obj: str, verbose: bool = False) -> None:
+    """One source to an object file.  With the matrix kernels' main loop in it, the assembly that the object is made
+    of is checked first (lds_reads)."""
+    hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
+    cmd = [hipcc] + [f for f in HIPCC_FLAGS if f != "-shared"] + ["-c", source, "-o", obj]
+    with open(source) as f:
+        checked = '#include "matmul.hpp"' in f.read()
+    _run(cmd + ["-save-temps=obj"] if checked else cmd, verbose)
+    if checked:
+        stem = os.path.splitext(os.path.basename(source))[0]
+        made = os.path.join(os.path.dirname(obj), f"{stem}-hip-amdgcn-amd-amdhsa-gfx950.s")
+        with open(made) as f:
+            lds_reads.check(f.read(), os.path.basename(source))
+
+
 def build_hip(verbose: bool = False) -> str:
     """The sources side by side, then one link (one after the other they take four times as long)."""
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
-    compile_flags = [f for f in HIPCC_FLAGS if f != "-shared"]
     jobs = max(1, min(8, os.cpu_count() or 1, int(os.environ.get("MAX_JOBS", "8") or 8)))
     with tempfile.TemporaryDirectory() as tmp, ThreadPoolExecutor(jobs) as pool:
         objects = [os.path.join(tmp, s + ".o") for s in SOURCES]
         # (the longest first)
         order = sorted(range(len(SOURCES)), key=lambda i: -os.path.getsize(os.path.join(CSRC, SOURCES[i])))
-        todo = [pool.submit(_run, [hipcc] + compile_flags + ["-c", os.path.join(CSRC, SOURCES[i]), "-o", objects[i]],
-                            verbose) for i in order]
+        todo = [pool.submit(compile_source, os.path.join(CSRC, SOURCES[i]), objects[i], verbose) for i in order]
         for t in todo:
             t.result()
         _run([hipcc] + HIPCC_FLAGS + ["-o", OUT] + objects, verbose)

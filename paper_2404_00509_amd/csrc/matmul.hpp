@@ -21,8 +21,8 @@
 //
 // Fragment reads are inline assembly, so that the compiler does not make each of them wait for every
 // direct load in flight; the code waits on lgkmcnt itself before it uses what was read, in straight lines, and
-// a test goes through the assembly for registers that are touched in between (spilled or moved, as under
-// more register pressure they are).
+// every build goes through the assembly of the library for registers that are touched in between (spilled or moved,
+// as under more register pressure they are) and refuses them.
 //
 // What bounds it.  A slice of a 256 x 256 tile takes 1.62 us on the 256 compute units together (1.3 PFLOP/s): its
 // multiplies alone take 1.00 us at 2.28 GHz, with the reads beside them 1.31 us at 1.8 GHz, with the loads too 1.62 us at
