@@ -406,7 +406,8 @@ int mae_dropout(const mae_dropout_desc* d, void* y, void* hip_stream);
  *
  * For every row x of D values: mean, rstd = 1 / sqrt(mean((x - mean)^2) + eps), h = (x - mean) rstd,
  *   y = h * weight + bias
- * Statistics are single precision, from two passes over registers.  Backward, with G = grad_y * weight:
+ * Statistics are single precision, from two passes over registers (a row whose sum or sum of squares is beyond the
+ * largest float has none).  Backward, with G = grad_y * weight:
  *   grad_x = rstd (G - mean(G) - h mean(G h)),  grad_weight = sum over rows of grad_y h,
  *   grad_bias = sum over rows of grad_y
  * The sums over rows have a fixed order (two calls give the same bits).

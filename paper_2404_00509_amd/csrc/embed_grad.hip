@@ -45,7 +45,8 @@ __device__ inline u32x4 filtered(u32x4 v, int filter) {
 
 // Part s of the sums: weight_acc[s][e][d], pos_acc[s][e][l].
 // In a product with zeros an infinity of one position is a NaN in all others (0 * inf).  That is how it is noticed: then the
-// tile is made again from the finite values, and infinities and NaN are added to the sums of their own positions.
+// tile is made again from the finite values, and infinities and NaN are added to the sums of their own positions (three
+// passes without loads in flight: 200,704 rows of NaN, 768 -> 768, 2.3 ms instead of 0.27; nothing where all is finite).
 template <int TM, int TN, int WGM, int WGN>
 __global__ __launch_bounds__(64 * WGM * WGN) void embed_products_kernel(EmbedGradArgs a) {
   using T = Tile<TM, TN, WGM, WGN, false, false>;

@@ -12,8 +12,8 @@
 // weight, bias and its share of their gradients in registers; sums over lanes go through DPP moves, not LDS.  The
 // shares of a workgroup are added through LDS, those of the workgroups by a second kernel in a fixed order, in double
 // precision, so results do not depend on scheduling.
-// 204,800 x 768 in bf16: forward 122 us (630 MB, 5.2 TB/s; 215 us without the loads ahead and with shuffles through LDS),
-// backward 172 + 6 us (945 MB, 5.3 TB/s); a copy of several GB runs at 4.7 TB/s on this card.
+// 204,800 x 768 in bf16: forward 123 us (630 MB, 5.1 TB/s; 215 us without the loads ahead and with shuffles through LDS),
+// backward 185 us (945 MB, 5.1 TB/s), 6 of them for the join; a copy of several GB runs at 4.7 TB/s on this card.
 #include "mae_device.hpp"
 #include "mae_kernels.hpp"
 
