@@ -1,6 +1,7 @@
 """Compile the HIP library for gfx950 in-tree: ``python -m paper_2404_00509_amd.build``."""
 from __future__ import annotations
 
+import glob
 import os
 import subprocess
 import sys
@@ -45,8 +46,10 @@ def compile_source(source: str, obj: str, verbose: bool = False) -> None:
     _run(cmd + ["-save-temps=obj"] if checked else cmd, verbose)
     if checked:
         stem = os.path.splitext(os.path.basename(source))[0]
-        made = os.path.join(os.path.dirname(obj), f"{stem}-hip-amdgcn-amd-amdhsa-gfx950.s")
-        with open(made) as f:
+        made = glob.glob(os.path.join(os.path.dirname(obj), stem + "-*gfx950*.s"))
+        if len(made) != 1:
+            raise RuntimeError(f"{stem}: the compiler left {len(made)} assembly files of the device code, expected one")
+        with open(made[0]) as f:
             lds_reads.check(f.read(), os.path.basename(source))
 
 

@@ -124,6 +124,7 @@ __device__ inline int half_exponent(int32_t peak) {
   const int e = (peak >> 7) - 127;  // 2^e <= the largest value < 2^(e + 1)
   return min(14 - e, 126);
 }
+
 __device__ inline uint32_t half_pair(float lo, float hi) {
   typedef float in2 __attribute__((ext_vector_type(2)));
   typedef _Float16 out2 __attribute__((ext_vector_type(2)));
@@ -313,9 +314,9 @@ struct Logits : Tile<TM, TN, WGM, WGN, true, true> {
         }
   }
 
-  // Rows 32 j .. + 31 of a wavefront's values as fp16 to g (as bf16, times `down`: kWide).  A lane has every second group of four classes of its row: the
-  // halves of the wavefront swap theirs, so that each has groups of eight, 16 bytes.  (Through strips of LDS, 256
-  // bytes along a row at a time: 3 % of a call over 32,003 classes more.)
+  // Rows 32 j .. + 31 of a wavefront's values as fp16 to g (kWide: as bf16, times `down`).  A lane has every second group of
+  // four classes of its row: the halves of the wavefront swap theirs, so that each has groups of eight, 16 bytes.  (Through
+  // strips of LDS, 256 bytes along a row at a time: 3 % of a call over 32,003 classes more.)
   template <int j, bool kWide = false>
   __device__ static inline void store_block(const ClassArgs& a, const Place& at, int wave, int lane,
                                             const f32x16 (&acc)[TM][TN], float down = 1.f) {
